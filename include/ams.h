@@ -46,7 +46,12 @@ typedef enum {
   AMS_ERR_HIP = 4                  /* a HIP launch reported an error                      */
 } ams_status;
 
-typedef enum { AMS_F32 = 0, AMS_BF16 = 1 } ams_dtype;
+typedef enum {
+  AMS_F32 = 0,
+  AMS_BF16 = 1,
+  AMS_INT8 = 2, /* ams_cache only: one-byte codes with a scale per block, see there      */
+  AMS_E4M3 = 3  /* ams_cache only: the 8-bit float of 4 exponent and 3 mantissa bits      */
+} ams_dtype;
 
 /* Plug-in base scorer g (Sec. 3.3 "In-Segment Selection with a Plug-and-Play
  * Scorer").  The mass that places segments always comes from the mean
@@ -311,6 +316,137 @@ int ams_compact(const ams_params* p, const ams_kv_view* src, const int32_t* idx,
 int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t* seq_lens,
                       const void* q, float* credit, const ams_kv_view* dst, float* credit_dst,
                       int32_t* idx, int32_t* n_kept, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ---- Between two events: new rows, attention, eviction, caches in 8 bits ----
+ *
+ * ams_cache - a cache of any element type.  kv_dtype rows (dtype == p->kv_dtype; the scales are
+ * ignored), or one-byte codes with one fp32 scale for K and one for V per BLOCK: 16 consecutive
+ * positions (16 j .. 16 j + 15) of one (layer, sequence, KV head), which is a page of the paged layout.
+ * A row's values are code * scale.
+ *   kv        k, v: kv_dtype rows, or codes in the same layouts, one byte each; 16-byte aligned;
+ *             paged: n_slots a multiple of 16 for codes
+ *   k_scale, v_scale  [dev] fp32; dense [layers, batch, kv_heads, ceil(t_capacity / 16)], paged
+ *             [layers, n_slots / 16, kv_heads]
+ * The scale that the library's writers give a block whose largest magnitude is a, with M = 127
+ * (AMS_INT8) or 448 (AMS_E4M3): 0 for a = 0, NaN for a value that is infinite or no number (the whole
+ * block is NaN then, its codes are 0), else 2^max(e, -120) with the least e for which a <= M * 2^e.  The
+ * code is the nearest to value / scale, of two equally near ones the even one.  Powers of two: the
+ * quotient is exact, every value of the cache is a bf16 number, and a scale that grows when rows are
+ * appended costs the rows that are there at most half a step each time, of steps that at least double:
+ * together less than one step of the final scale.  The readers take any finite scale.  Codes of
+ * AMS_E4M3 that are no number are not written by the library; a caller's own make the sums they enter NaN.
+ * A block table entry outside the pool is read as the nearest page and never written through.
+ */
+typedef struct {
+  ams_kv_view kv;
+  int32_t dtype;  /* ams_dtype of k and v */
+  float* k_scale;
+  float* v_scale;
+} ams_cache;
+
+/* Rotary positions: the angle of pair i at position n is n * freq[i]; a pair (a, b) becomes gain * (a cos - b sin,
+ * b cos + a sin).  Plain data, [host]; read before ams_append returns. */
+typedef enum {
+  AMS_ROPE_HALF = 0,       /* pair i: channels i and i + rot_dim / 2 */
+  AMS_ROPE_INTERLEAVED = 1 /* pair i: channels 2 i and 2 i + 1       */
+} ams_rope_layout;
+typedef enum {
+  AMS_ROPE_PLAIN = 0,   /* f_i = base^(-2 i / rot_dim)                                                          */
+  AMS_ROPE_LINEAR = 1,  /* f_i / factor                                                                         */
+  AMS_ROPE_BASE = 2,    /* with base * factor^(rot_dim / (rot_dim - 2)) for base; rot_dim > 2                   */
+  AMS_ROPE_BY_PARTS = 3 /* f_i * (c + (1 - c) / factor), c = clamp((r - slow) / (fast - slow), 0, 1),
+                           r = original_len * f_i / (2 pi): the turns over the original context                 */
+} ams_rope_scaling;
+typedef struct {
+  int32_t layout;  /* ams_rope_layout                                                                     */
+  int32_t rot_dim; /* channels 0 .. rot_dim - 1 rotate, the others pass; even, 0 .. head_dim; 0 = none      */
+  float gain;      /* factor on the rotated channels (an attention factor for long contexts); 1 = none    */
+  double freq[64]; /* radians per position of pair i                                                      */
+} ams_rope;
+
+/* ams_rope_init - fills *out ([host], pure).  AMS_ERR_INVALID_ARG for a null pointer, an odd or negative rot_dim or one above 128,
+ * base <= 0, factor < 1 where the scaling uses it, original_len < 1 or fast <= slow with AMS_ROPE_BY_PARTS, a gain that is not finite. */
+int ams_rope_init(ams_rope* out, int32_t layout, int32_t rot_dim, double base, int32_t scaling, double factor,
+                  int32_t original_len, double slow, double fast, float gain);
+
+/* The tokens that ams_append takes.  Plain data, [host]. */
+typedef struct {
+  const void* q; /* [dev] kv_dtype; row of head i of token w of (l, b): q + ((l * batch + b) * n_new + w) * q_stride
+                    + i * head_dim elements, kv_heads * group heads; k, v: kv_heads heads.  NULL: no queries          */
+  const void* k;
+  const void* v;
+  int64_t q_stride, k_stride, v_stride; /* elements from one token to the next; pointers and strides multiples of 16 bytes */
+  const void* q_weight;                 /* [dev] kv_dtype [head_dim]; NULL: queries are not normalised               */
+  const void* k_weight;                 /* the same for keys                                                         */
+  float norm_eps;                       /* >= 0, finite                                                              */
+  const int32_t* positions; /* [dev] [batch]: position of the first new token, the others follow; NULL: its place in the cache */
+  int32_t n_new;            /* tokens per sequence, >= 1                                                             */
+} ams_new_tokens;
+
+/*
+ * ams_append - n_new tokens behind the seq_lens[b] rows of every sequence, in one pass: every query and key is normalised
+ * over its head (x / sqrt(mean(x^2) + norm_eps) * weight; left out without a weight), then rotated, keys and values are
+ * written to rows seq_lens[b] .. of the cache and the queries to q_out in the layout of ams_score and ams_attend.
+ * The angles are formed in 64 bits and reduced there; what is written is rounded once (keys that go to 8 bits are normalised and rotated
+ * in 64 bits).  Of p: the sizes, kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are
+ * not written (a full sequence takes nothing), so seq_lens[b] = t_max leaves a sequence of a padded batch out.
+ * A block of an 8-bit cache that already holds rows takes the larger of its scale and that of the new rows; where it
+ * grows the rows that are there are rounded again.  A block that the call begins takes nothing from its old scale.
+ *   q_out    [dev] [layers, batch, kv_heads * group, n_new, head_dim] kv_dtype, all of it written; NULL when x->q is
+ *   lens_out [dev] [batch] min(seq_lens[b] + n_new, t_max), or NULL; not seq_lens itself
+ * rope NULL or rot_dim 0: no rotation.
+ */
+int ams_append(const ams_params* p, const ams_new_tokens* x, const ams_rope* rope, const int32_t* seq_lens, void* q_out,
+               const ams_cache* dst, int32_t* lens_out, void* stream);
+
+/* Bytes of scratch of ams_attend and ams_evict for these parameters ([host], pure; 0: bad parameters). */
+size_t ams_attend_workspace_bytes(const ams_params* p);
+size_t ams_evict_workspace_bytes(const ams_params* p);
+
+/*
+ * ams_attend - attention of the query window over a cache in 8 bits, and the weights that its positions received.
+ *   s[n][t] = q_n . k_t / sqrt(D), p = softmax over the positions that n sees, out_n = sum_t p[n][t] v_t,
+ *   lse_n = ln sum_t exp(s[n][t]),  weights_out[t] = weights_in[t] + sum_n p[n][t]   (n: the unit's G * W queries)
+ * p->causal == 0: every query sees 0 .. T-1; 1: query w sits at T-W+w and sees 0 .. T-W+w.  A query that sees nothing
+ * (T = 0; before position 0) has out 0 and lse -inf and adds no weight.
+ * Of p: the sizes, kv_dtype (of q and out), causal, t_max, t_stride; group * window <= 256 (AMS_ERR_UNSUPPORTED).
+ *   src   AMS_INT8 or AMS_E4M3 (AMS_ERR_UNSUPPORTED otherwise)
+ *   q     [dev] [layers, batch, kv_heads * group, window, head_dim] kv_dtype; out likewise, written
+ *   lse   [dev] fp32 [layers, batch, kv_heads * group, window], or NULL
+ *   weights_in, weights_out  [dev] fp32 [units, t_stride]; entries 0 .. T-1 read and written, the others left as they are; weights_in
+ *         NULL: zeros; weights_out NULL: no weights wanted; they may be the same array
+ *   ws    [dev] scratch of at least ams_attend_workspace_bytes(p)
+ * Codes times queries are exact products, summed in fp32; probabilities enter the second product as two bf16 terms (16 bits), three with
+ * fp32 queries.  Nothing depends on the order in which workgroups run.
+ */
+int ams_attend(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const void* q, void* out, float* lse,
+               const float* weights_in, float* weights_out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ams_recode - ams_compact between caches of different element types: rows of kv_dtype to 8 bits, 8 bits to rows, 8 bits to 8 bits.
+ *   idx != NULL: row j < n_kept[unit] of the destination is row idx[unit * budget + j] of the source (an index
+ *         outside [0, t_max) gives a row of zeros), credit as in ams_compact; seq_lens is not read
+ *   idx == NULL: rows 0 .. seq_lens[b]-1 in place order; n_kept, credit_src and credit_dst are not used
+ * Every block takes a scale of its own (ams_cache); rows behind the last one are left as they are.  src and
+ * dst must not overlap.  Two caches of kv_dtype: AMS_ERR_UNSUPPORTED (ams_compact does that).
+ */
+int ams_recode(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const int32_t* idx, const int32_t* n_kept,
+               const ams_cache* dst, const float* credit_src, float* credit_dst, void* stream);
+
+/*
+ * ams_evict - back to the budget by accumulated weight: of T positions min(budget, T) stay, the first min(n_sink, kept), the
+ * last min(n_last, kept - sinks), and of the others those of largest weights[t] (equal ones: lower position first; NaN ranks
+ * below everything; -0 equals 0).  Their rows go to dst in order (ams_recode's rules; both caches of kv_dtype: copied).
+ *   weights     [dev] fp32 [units, t_stride], as ams_attend accumulates them
+ *   weights_out [dev] fp32 [units, t_stride]: those of the kept positions, then zeros up to t_max; not weights itself
+ *   idx [dev] int32 [units, budget] kept positions, ascending, then -1; n_kept [dev] int32 [units]
+ *   lens_out [dev] [batch] min(budget, seq_lens[b]), or NULL; not seq_lens itself
+ *   ws  [dev] scratch of at least ams_evict_workspace_bytes(p)
+ * Of p: the sizes, kv_dtype, t_max, t_stride, budget, n_sink, n_last.
+ */
+int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const float* weights, const ams_cache* dst,
+              float* weights_out, int32_t* idx, int32_t* n_kept, int32_t* lens_out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,16 +19,20 @@ LIB_PATH = os.path.join(_HERE, "libams.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE_TOO_SMALL, ERR_HIP = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
+INT8, E4M3 = 2, 3                     # element types of a cache only (cache_view)
 SCORER_LAST_QUERY, SCORER_MEAN_WINDOW, SCORER_KEYDIFF, SCORER_EXPECTED, SCORER_EXTERNAL = 0, 1, 2, 3, 4
 SCORER_EXPECTED_VNORM = 5
 SCORER_REDUNDANCY = 6
 LAYOUT_DENSE, LAYOUT_PAGED = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
 SCORE_PATH_AUTO, SCORE_PATH_TWO_SWEEPS, SCORE_PATH_ONE_READ, SCORE_PATH_ONE_LAUNCH = 0, 1, 2, 3
 
 EXPORTS = ("ams_status_string", "ams_workspace_bytes", "ams_workspace_layout", "ams_profile_begin",
            "ams_profile_end", "ams_debug_set_wait_limit", "ams_score",
            "ams_ema_update", "ams_mass_segment", "ams_mass_segment_static", "ams_select", "ams_compact",
-           "ams_compress_step")
+           "ams_compress_step", "ams_rope_init", "ams_append", "ams_attend_workspace_bytes", "ams_attend", "ams_recode",
+           "ams_evict_workspace_bytes", "ams_evict")
 
 
 class AmsError(RuntimeError):
@@ -64,6 +68,21 @@ class WorkspaceView(C.Structure):
                 ("seg_mass", C.c_size_t), ("quota", C.c_size_t)]
 
 
+class Cache(C.Structure):
+    """A cache of any element type (cache_view).  Keeps its tensors alive; `device` is theirs."""
+    _fields_ = [("kv", KvView), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rot_dim", C.c_int32), ("gain", C.c_float), ("freq", C.c_double * 64)]
+
+
+class NewTokens(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("norm_eps", C.c_float),
+                ("positions", C.c_void_p), ("n_new", C.c_int32)]
+
+
 _lib = None
 
 
@@ -89,8 +108,17 @@ def lib() -> C.CDLL:
         l.ams_compact.argtypes = [P, V, p, p, V, p, p, p]
         l.ams_compress_step.argtypes = [P, V, p, p, p, V, p, p, p, p, C.c_size_t, p]
         l.ams_profile_end.argtypes = [p, C.c_int, C.POINTER(C.c_char_p), C.POINTER(C.c_float)]
+        K, d = C.POINTER(Cache), C.c_double
+        l.ams_rope_init.argtypes = [C.POINTER(Rope), C.c_int32, C.c_int32, d, C.c_int32, d, C.c_int32, d, d, C.c_float]
+        l.ams_append.argtypes = [P, C.POINTER(NewTokens), C.POINTER(Rope), p, p, K, p, p]
+        l.ams_attend.argtypes = [P, K, p, p, p, p, p, p, p, C.c_size_t, p]
+        l.ams_recode.argtypes = [P, K, p, p, p, K, p, p, p]
+        l.ams_evict.argtypes = [P, K, p, p, K, p, p, p, p, p, C.c_size_t, p]
         for name in EXPORTS[2:]:
             getattr(l, name).restype = C.c_int
+        for name in ("ams_attend_workspace_bytes", "ams_evict_workspace_bytes"):
+            getattr(l, name).restype = C.c_size_t
+            getattr(l, name).argtypes = [P]
         _lib = l
     return _lib
 
@@ -212,6 +240,165 @@ def ams_compress_step(p, src, seq_lens, q, credit, dst, credit_dst, idx, n_kept,
     _check(lib().ams_compress_step(C.byref(p), C.byref(src), _ptr(seq_lens), _ptr(q), _ptr(credit),
                                    C.byref(dst), _ptr(credit_dst), _ptr(idx), _ptr(n_kept), _ptr(ws),
                                    ws.numel() * ws.element_size(), _stream(stream)), "ams_compress_step")
+
+
+# ---- between two events: new rows, attention, eviction, caches in 8 bits ----
+
+_CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: INT8, torch.float8_e4m3fn: E4M3}
+BLOCK = 16                             # positions that share a scale
+
+
+def scale_shape(k: torch.Tensor):
+    """Shape of k_scale and v_scale of a cache whose keys have the shape of `k` (dense or paged)."""
+    if k.dim() == 5:
+        return tuple(k.shape[:3]) + (-(-k.shape[3] // BLOCK),)
+    return (k.shape[0], k.shape[1] // BLOCK, k.shape[2])
+
+
+def cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+               v_scale: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None) -> Cache:
+    """A cache of rows (bf16, fp32) or of codes (int8, float8_e4m3fn) with their scales: k, v [L, B, H, t_capacity, D], or, with a
+    block table (int32 [B, max_blocks]), pools [L, n_slots, H, D]."""
+    tensors = [t for t in (k, v, k_scale, v_scale, block_table) if t is not None]
+    if any(not t.is_cuda or t.device != k.device for t in tensors):
+        raise ValueError("a cache's tensors lie on one GPU")
+    if any(not t.is_contiguous() for t in tensors):
+        raise ValueError("contiguous tensor expected")
+    if k.dtype not in _CACHE_DTYPES or k.dtype != v.dtype or k.shape != v.shape or k.dim() != (5 if block_table is None else 4):
+        raise ValueError("k and v: one shape, one element type of bf16, fp32, int8, float8_e4m3fn; five dimensions, paged four")
+    dtype = _CACHE_DTYPES[k.dtype]
+    if dtype in (INT8, E4M3):
+        for t in (k_scale, v_scale):
+            if t is None or t.dtype != torch.float32 or tuple(t.shape) != scale_shape(k):
+                raise ValueError(f"fp32 scales of shape {scale_shape(k)} expected")
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError("rows of bf16 or fp32 have no scales")
+    if block_table is not None and (block_table.dtype != torch.int32 or block_table.dim() != 2):
+        raise ValueError("int32 block table [batch, max_blocks] expected")
+    kv = dense_view(k, v) if block_table is None else paged_view(k, v, block_table)
+    c = Cache(kv, dtype, k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None)
+    c.tensors, c.device, c.k_dtype = tensors, k.device, k.dtype
+    c.lead = tuple(k.shape[:3]) if block_table is None else (k.shape[0], block_table.shape[0], k.shape[2])
+    c.head_dim = k.shape[-1]
+    return c
+
+
+def make_rope(rot_dim: int, layout: int = ROPE_HALF, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+              original_len: int = 0, slow: float = 1.0, fast: float = 32.0, gain: float = 1.0) -> Rope:
+    r = Rope()
+    _check(lib().ams_rope_init(C.byref(r), layout, rot_dim, base, scaling, factor, original_len, slow, fast, gain), "ams_rope_init")
+    return r
+
+
+def _cache_for(p: Params, c: Cache):
+    if c.lead != (p.n_layers, p.batch, p.n_kv_heads) or c.head_dim != p.head_dim:
+        raise ValueError(f"a cache of {c.lead} heads of {c.head_dim} channels does not fit the parameters")
+
+
+def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, device: torch.device, what: str):
+    """Pointer of a contiguous tensor of at least `numel` elements on the call's GPU; None stays None."""
+    if t is None:
+        return None
+    if t.device != device or t.dtype != dtype or t.numel() < numel or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {dtype} tensor of at least {numel} elements on {device} expected")
+    return t.data_ptr()
+
+
+def _launch(fn, what: str, device: torch.device, stream, *args):
+    """Calls fn on the cache's GPU, whichever is current, and on that GPU's current stream unless one is given."""
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream(stream))
+    _check(rc, what)
+
+
+def _rows_dtype(p: Params) -> torch.dtype:
+    return torch.float32 if p.kv_dtype == F32 else torch.bfloat16
+
+
+def _token_rows(t: torch.Tensor, p: Params, heads: int, n_new: int, dtype, device, what: str):
+    """(pointer, elements from token to token) of [L, B, n_new, heads, D]: any slice of a projection's output along the heads."""
+    s = t.stride()
+    if (t.device != device or t.dtype != dtype or t.shape != (p.n_layers, p.batch, n_new, heads, p.head_dim) or s[4] != 1
+            or (heads > 1 and s[3] != p.head_dim)):
+        raise ValueError(f"{what}: {dtype} [layers, batch, new, {heads}, {p.head_dim}] on {device} with contiguous heads expected")
+    for stride, n, want in ((s[1], p.batch, s[2] * n_new), (s[0], p.n_layers, s[2] * n_new * p.batch)):
+        if n > 1 and n_new > 1 and stride != want:
+            raise ValueError(f"{what}: one stride from token to token expected")
+    step = s[2]
+    if n_new == 1:                      # the tokens are those of the batch, then of the layers
+        step = s[1] if p.batch > 1 else s[0] if p.n_layers > 1 else max(s[2], heads * p.head_dim)
+        if p.batch > 1 and p.n_layers > 1 and s[0] != step * p.batch:
+            raise ValueError(f"{what}: one stride from token to token expected")
+    elif n_new > 1 and p.batch == 1 and p.n_layers > 1 and s[0] != s[2] * n_new:
+        raise ValueError(f"{what}: one stride from token to token expected")
+    return t.data_ptr(), step
+
+
+def ams_append(p, q, k, v, q_weight, k_weight, norm_eps, rope, positions, seq_lens, q_out, dst, lens_out=None, stream=None):
+    """q [L, B, n_new, H * G, D] (or None, q_out too), k, v [L, B, n_new, H, D]; rope, the weights, positions and lens_out may be None."""
+    _cache_for(p, dst)
+    dev, rows, n_new = dst.device, _rows_dtype(p), k.shape[2]
+    HQ = p.n_kv_heads * p.group
+    qp, qs = _token_rows(q, p, HQ, n_new, rows, dev, "q") if q is not None else (None, 0)
+    kp, ks = _token_rows(k, p, p.n_kv_heads, n_new, rows, dev, "k")
+    vp, vs = _token_rows(v, p, p.n_kv_heads, n_new, rows, dev, "v")
+    x = NewTokens(qp, kp, vp, qs, ks, vs, _arg(q_weight, rows, p.head_dim, dev, "q_weight"),
+                  _arg(k_weight, rows, p.head_dim, dev, "k_weight"), norm_eps,
+                  _arg(positions, torch.int32, p.batch, dev, "positions"), n_new)
+    _launch(lib().ams_append, "ams_append", dev, stream, C.byref(p), C.byref(x), C.byref(rope) if rope is not None else None,
+            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"),
+            _arg(q_out, rows, p.n_layers * p.batch * HQ * n_new * p.head_dim, dev, "q_out"), C.byref(dst),
+            _arg(lens_out, torch.int32, p.batch, dev, "lens_out"))
+
+
+def ams_attend_workspace_bytes(p: Params) -> int:
+    return int(lib().ams_attend_workspace_bytes(C.byref(p)))
+
+
+def ams_attend(p, src, seq_lens, q, out, ws, lse=None, weights_in=None, weights_out=None, stream=None):
+    _cache_for(p, src)
+    dev, rows = src.device, _rows_dtype(p)
+    n = p.units * p.group * p.window
+    _launch(lib().ams_attend, "ams_attend", dev, stream, C.byref(p), C.byref(src),
+            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"), _arg(q, rows, n * p.head_dim, dev, "q"),
+            _arg(out, rows, n * p.head_dim, dev, "out"), _arg(lse, torch.float32, n, dev, "lse"),
+            _arg(weights_in, torch.float32, p.units * p.t_stride, dev, "weights_in"),
+            _arg(weights_out, torch.float32, p.units * p.t_stride, dev, "weights_out"),
+            _arg(ws, torch.uint8, 0, dev, "ws"), ws.numel())
+
+
+def ams_recode(p, src, seq_lens, dst, idx=None, n_kept=None, credit_src=None, credit_dst=None, stream=None):
+    _cache_for(p, src)
+    _cache_for(p, dst)
+    dev = src.device
+    if dst.device != dev:
+        raise ValueError("both caches lie on one GPU")
+    _launch(lib().ams_recode, "ams_recode", dev, stream, C.byref(p), C.byref(src),
+            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"), _arg(idx, torch.int32, p.units * p.budget, dev, "idx"),
+            _arg(n_kept, torch.int32, p.units, dev, "n_kept"), C.byref(dst),
+            _arg(credit_src, torch.float32, p.units * p.t_stride, dev, "credit_src"),
+            _arg(credit_dst, torch.float32, p.units * p.budget, dev, "credit_dst"))
+
+
+def ams_evict_workspace_bytes(p: Params) -> int:
+    return int(lib().ams_evict_workspace_bytes(C.byref(p)))
+
+
+def ams_evict(p, src, seq_lens, weights, dst, weights_out, idx, n_kept, ws, lens_out=None, stream=None):
+    _cache_for(p, src)
+    _cache_for(p, dst)
+    dev = src.device
+    if dst.device != dev:
+        raise ValueError("both caches lie on one GPU")
+    _launch(lib().ams_evict, "ams_evict", dev, stream, C.byref(p), C.byref(src),
+            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"),
+            _arg(weights, torch.float32, p.units * p.t_stride, dev, "weights"), C.byref(dst),
+            _arg(weights_out, torch.float32, p.units * p.t_stride, dev, "weights_out"),
+            _arg(idx, torch.int32, p.units * p.budget, dev, "idx"), _arg(n_kept, torch.int32, p.units, dev, "n_kept"),
+            _arg(lens_out, torch.int32, p.batch, dev, "lens_out"), _arg(ws, torch.uint8, 0, dev, "ws"), ws.numel())
 
 
 @dataclass

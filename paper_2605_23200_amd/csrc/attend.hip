@@ -1,0 +1,551 @@
+// Attention over a cache of 8 bits (ams_attend).
+//
+// One wave takes 32 positions at a time: K as 16x16x32 tiles with the positions as rows and the queries as columns,
+// S^T = K Q^T, so that a lane ends with 2 x 4 logits of ONE query (column lane % 16) at positions 4 (lane / 16) + 0..3 of both
+// tiles.  That is already the layout in which the second product, O^T = V^T P^T over the same 32 positions, wants P (its k index
+// runs over the positions in any order both operands share), so probabilities never leave the lane.  V is read as bytes of
+// 8 positions per lane and turned there: one v_perm per two elements, which the conversion to bf16 needs anyway.  Codes are bf16 numbers,
+// so q.k has exact products; the scales of the two blocks of 16 positions go to the logits and to the probabilities.
+// Softmax: a running reference per query that is moved (and O rescaled) only when a logit exceeds it by 2^8; P and the
+// sums are then at most 2^8 per position, far inside bf16's and fp32's range.
+// No LDS until the four waves of a workgroup (which take the steps of their split in turn) join their sums, fixed order.
+// The splits of a long axis are joined by attend_join_kernel, again in fixed order.
+//
+// Weights: with up to 16 queries the logits go to scratch (4 N bytes a position, written and read once, against 2 D of K and V)
+// and the join turns them into probabilities; beyond that K is read a second time (attend_weights_kernel).
+#include "cache.h"
+#include "score_tile.h"
+
+namespace ams {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kStep = 32;                 // positions per wave and step
+constexpr float kSlack = 8.f;             // log2 by which a logit may exceed the reference
+constexpr float kLowest = -1e38f;         // reference before any logit
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+
+// Two codes of a word, bytes 2 HALF and 2 HALF + 1, as bf16.
+template <int EL, int HALF>
+__device__ __forceinline__ uint32_t two_codes(uint32_t w) {
+  if constexpr (EL == EL_INT8) {
+    const float a = (float)(int8_t)(w >> (16 * HALF)), b = (float)(int8_t)(w >> (16 * HALF + 8));
+    return high_halves(__float_as_uint(a), __float_as_uint(b));
+  } else {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, HALF);
+    return __builtin_bit_cast(uint32_t, c);
+  }
+}
+// Eight codes -> the operand of one product.
+template <int EL>
+__device__ __forceinline__ bf16x8 eight_codes(uint32_t lo, uint32_t hi) {
+  const uint4 r = make_uint4(two_codes<EL, 0>(lo), two_codes<EL, 1>(lo), two_codes<EL, 0>(hi), two_codes<EL, 1>(hi));
+  return __builtin_bit_cast(bf16x8, r);
+}
+// Word w[j] holds elements 0..3 of position j: the eight positions of element E.
+template <int EL, int E>
+__device__ __forceinline__ void turn_pair(const uint32_t (&w)[8], bf16x8& first, bf16x8& second) {  // elements 2 E, 2 E + 1
+  uint32_t a[4], b[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (EL == EL_INT8) {
+      a[j] = high_halves(__float_as_uint((float)(int8_t)(w[2 * j] >> (16 * E))), __float_as_uint((float)(int8_t)(w[2 * j + 1] >> (16 * E))));
+      b[j] = high_halves(__float_as_uint((float)(int8_t)(w[2 * j] >> (16 * E + 8))),
+                         __float_as_uint((float)(int8_t)(w[2 * j + 1] >> (16 * E + 8))));
+    } else {
+      const uint32_t x = two_codes<EL, E>(w[2 * j]), y = two_codes<EL, E>(w[2 * j + 1]);
+      a[j] = low_halves(x, y);
+      b[j] = high_halves(x, y);
+    }
+  }
+  first = __builtin_bit_cast(bf16x8, make_uint4(a[0], a[1], a[2], a[3]));
+  second = __builtin_bit_cast(bf16x8, make_uint4(b[0], b[1], b[2], b[3]));
+}
+
+// 2^x to an ulp; results below 2^-126 are 0, which no sum here notices.
+__device__ __forceinline__ float power_of_two(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ floatx4 mma(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// Over the four lanes that hold one query.
+__device__ __forceinline__ float query_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float query_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// Channel of element 0 of the 8 that lane group g feeds to product i of q.k: 16 bytes of a K row per load.
+__device__ __forceinline__ int k_channel(int i, int g) { return 64 * (i >> 1) + 16 * g + 8 * (i & 1); }
+
+// The query operand of rows row0 + 16 r + lane % 16, as TERMS bf16 terms.
+template <bool BF16, int HD, int R>
+struct Queries {
+  static constexpr int TERMS = BF16 ? 1 : 3, STEPS = HD / 32;
+  bf16x8 x[R][STEPS][TERMS];
+  __device__ __forceinline__ void load(const char* unit_q, int row0, int N, int lane) {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int n = row0 + r * 16 + (lane & 15);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int d = k_channel(i, g);
+        if constexpr (BF16) {
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (n < N) v = *(const uint4*)(unit_q + ((int64_t)n * HD + d) * 2);
+          x[r][i][0] = __builtin_bit_cast(bf16x8, v);
+        } else {
+          float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          if (n < N) load_eight<EL_F32>(unit_q + ((int64_t)n * HD + d) * 4, v);
+          uint32_t t[3][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) split2<true>(v[2 * j], v[2 * j + 1], t[0][j], t[1][j], t[2][j]);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) x[r][i][k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]));
+        }
+      }
+    }
+  }
+};
+
+// A block of K as the wave reads it: lane % 16 is the position, lane / 16 the 16 bytes of every 64.
+template <int HD>
+struct KTile {
+  uint4 w[HD / 64];
+  float scale;
+  // rows past the last one read that one again; a block past the last one likewise
+  __device__ __forceinline__ void load(const CacheDev& c, int l, int b, int h, int blk, int T, int lane) {
+    const int use = min(blk, (T - 1) / kBlockRows);
+    const Block k = block_at(c, l, b, h, use);
+    scale = c.scale[k.scale];
+    const char* row = k.row0 + min(lane & 15, T - 1 - use * kBlockRows) * k.stride + (lane >> 4) * 16;
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i) w[i] = *(const uint4*)(row + 64 * i);
+  }
+  template <int EL>
+  __device__ __forceinline__ bf16x8 operand(int i) const {
+    return (i & 1) ? eight_codes<EL>(w[i >> 1].z, w[i >> 1].w) : eight_codes<EL>(w[i >> 1].x, w[i >> 1].y);
+  }
+};
+
+// Two blocks of V: lane % 16 is the stretch of HD / 16 channels, word [j] of position 4 (lane / 16) + j % 4 of block j / 4.
+template <int HD>
+struct VTile {
+  static constexpr int WORDS = HD / 64;  // of 4 channels
+  uint32_t w[WORDS][8];
+  float scale[2];
+  __device__ __forceinline__ void load(const CacheDev& c, int l, int b, int h, int blk, int T, int lane) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int use = min(blk + j, (T - 1) / kBlockRows);
+      const Block v = block_at(c, l, b, h, use);
+      scale[j] = c.scale[v.scale];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const char* at = v.row0 + min((lane >> 4) * 4 + i, T - 1 - use * kBlockRows) * v.stride + (lane & 15) * (HD / 16);
+        if constexpr (WORDS == 2) {
+          const uint2 x = *(const uint2*)at;
+          w[0][4 * j + i] = x.x, w[1][4 * j + i] = x.y;
+        } else {
+          w[0][4 * j + i] = *(const uint32_t*)at;
+        }
+      }
+    }
+  }
+};
+
+// One split of one unit's positions for 16 R of its queries.
+template <int EL, bool BF16, int HD, int R>
+__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
+  constexpr int STEPS = HD / 32, TILES = HD / 16, TERMS = BF16 ? 1 : 3, PTERMS = BF16 ? 2 : 3;
+  constexpr int LD = HD + 4;  // row of the join in LDS
+  __shared__ __align__(16) float joint[kWaves][16][LD];
+  __shared__ float2 stat[kWaves][16];
+  const int unit = blockIdx.y, split = blockIdx.x, row0 = blockIdx.z * 16 * R;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int g = lane >> 4, c = lane & 15;
+  int l, b, h;
+  unit_coords(a.d, unit, l, b, h);
+  const int T = seq_len(a.d, a.seq_lens, b), N = a.d.N;
+  const int begin = split * a.chunk, end = min(T, begin + a.chunk);
+  if (begin >= T && split > 0) return;  // the join knows; split 0 of an empty sequence writes the zeros
+  Queries<BF16, HD, R> q;
+  q.load(a.q + (int64_t)unit * N * HD * (BF16 ? 2 : 4), row0, N, lane);
+  int limit[R];  // positions that the lane's query sees
+  int fewest = T;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int n = row0 + r * 16 + c;
+    limit[r] = a.causal ? T - a.d.W + 1 + n % a.d.W : T;
+    if (a.causal) fewest = T - a.d.W + 1;
+  }
+  floatx4 o[R][TILES];
+  float m[R], sum[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = kLowest, sum[r] = 0.f;
+#pragma unroll
+    for (int e = 0; e < TILES; ++e) o[r][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float to_log2 = kLog2E / sqrtf((float)HD);
+  KTile<HD> kt[2];
+  VTile<HD> vt;
+  int at = begin + wave * kStep;
+  if (at < end) {
+    kt[0].load(a.k, l, b, h, at / kBlockRows, T, lane);
+    kt[1].load(a.k, l, b, h, at / kBlockRows + 1, T, lane);
+    vt.load(a.v, l, b, h, at / kBlockRows, T, lane);
+  }
+  for (; at < end; at += kWaves * kStep) {
+    floatx4 s[2][R];
+    float kscale[2], vscale[2];
+    VTile<HD> v = vt;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      kscale[j] = kt[j].scale * to_log2, vscale[j] = vt.scale[j];
+#pragma unroll
+      for (int r = 0; r < R; ++r) s[j][r] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const bf16x8 k = kt[j].template operand<EL>(i);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int t = TERMS - 1; t >= 0; --t) s[j][r] = mma(k, q.x[r][i][t], s[j][r]);
+      }
+    }
+    const int next = at + kWaves * kStep;
+    if (next < end) {
+      kt[0].load(a.k, l, b, h, next / kBlockRows, T, lane);
+      kt[1].load(a.k, l, b, h, next / kBlockRows + 1, T, lane);
+      vt.load(a.v, l, b, h, next / kBlockRows, T, lane);
+    }
+    const bool whole = at + kStep <= fewest;  // every query sees every position of the step
+    bf16x8 p[R][PTERMS];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float x[8];
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] = s[j >> 2][r][j & 3] * kscale[j >> 2];
+        if (!whole && at + (j >> 2) * 16 + 4 * g + (j & 3) >= limit[r]) x[j] = -INFINITY;
+        top = fmaxf(top, x[j]);
+      }
+      if (__any(top > m[r] + kSlack)) {
+        const float now = fmaxf(m[r], query_max(top)), shrink = power_of_two(m[r] - now);
+        m[r] = now;
+        sum[r] *= shrink;
+#pragma unroll
+        for (int e = 0; e < TILES; ++e) o[r][e] *= shrink;
+      }
+      if (R == 1 && a.stash && c < N) {
+        float* to = a.stash + (((int64_t)unit * ((a.d.t_max + 15) / 16) + at / 16) * N + c) * 16 + 4 * g;
+        *(float4*)to = make_float4(x[0], x[1], x[2], x[3]);
+        if (at + 16 < T) *(float4*)(to + N * 16) = make_float4(x[4], x[5], x[6], x[7]);
+      }
+      uint32_t t[3][4];
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        float p0 = power_of_two(x[j] - m[r]), p1 = power_of_two(x[j + 1] - m[r]);
+        sum[r] += p0 + p1;
+        p0 *= vscale[j >> 2], p1 *= vscale[j >> 2];
+        if (!whole) {  // a scale that is no number at a position that the query does not see
+          if (x[j] == -INFINITY) p0 = 0.f;
+          if (x[j + 1] == -INFINITY) p1 = 0.f;
+        }
+        t[0][j >> 1] = bf16_pair(p0, p1);
+        p0 -= __uint_as_float(t[0][j >> 1] << 16), p1 -= __uint_as_float(t[0][j >> 1] & 0xFFFF0000u);
+        t[1][j >> 1] = bf16_pair(p0, p1);
+        if constexpr (PTERMS == 3) {
+          p0 -= __uint_as_float(t[1][j >> 1] << 16), p1 -= __uint_as_float(t[1][j >> 1] & 0xFFFF0000u);
+          t[2][j >> 1] = bf16_pair(p0, p1);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < PTERMS; ++k) p[r][k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]));
+    }
+#pragma unroll
+    for (int w = 0; w < VTile<HD>::WORDS; ++w) {
+      bf16x8 e[4];
+      turn_pair<EL, 0>(v.w[w], e[0], e[1]);
+      turn_pair<EL, 1>(v.w[w], e[2], e[3]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int t = PTERMS - 1; t >= 0; --t) o[r][4 * w + k] = mma(e[k], p[r][t], o[r][4 * w + k]);
+    }
+  }
+  // the four waves together: 16 queries at a time, thread (query, stretch of HD / 16 channels)
+  const bool last = a.n_splits == 1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int n0 = row0 + r * 16;
+    if (n0 >= N) break;
+    if (r > 0) __syncthreads();
+    const float total = query_sum(sum[r]);
+    if (g == 0) stat[wave][c] = make_float2(m[r], total);
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4)  // the lane's rows 4 g + q4 of every tile: channels TILES (4 g + q4) + tile
+#pragma unroll
+      for (int e = 0; e < TILES; e += 4)
+        *(float4*)&joint[wave][c][TILES * (4 * g + q4) + e] = make_float4(o[r][e][q4], o[r][e + 1][q4], o[r][e + 2][q4], o[r][e + 3][q4]);
+    __syncthreads();
+    const int qr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * TILES, n = n0 + qr;
+    float top = stat[0][qr].x;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, stat[w][qr].x);
+    float x[TILES], all = 0.f;
+#pragma unroll
+    for (int e = 0; e < TILES; ++e) x[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = power_of_two(stat[w][qr].x - top);
+      all += f * stat[w][qr].y;
+#pragma unroll
+      for (int e = 0; e < TILES; ++e) x[e] = fmaf(f, joint[w][qr][d0 + e], x[e]);
+    }
+    if (n < N) {
+      const int64_t row = ((int64_t)unit * a.n_splits + split) * N + n;
+      if (threadIdx.x % 16 == 0) {
+        a.stats[row] = make_float2(top, all);
+        if (last && a.lse) a.lse[(int64_t)unit * N + n] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
+      }
+      if (last) {
+        const float inverse = all == 0.f ? 0.f : 1.f / all;
+        char* to = a.out + (((int64_t)unit * N + n) * HD + d0) * (BF16 ? 2 : 4);
+#pragma unroll
+        for (int e = 0; e < TILES; e += 4) {
+          const float y0 = x[e] * inverse, y1 = x[e + 1] * inverse, y2 = x[e + 2] * inverse, y3 = x[e + 3] * inverse;
+          if constexpr (BF16)
+            *(uint2*)(to + 2 * e) = make_uint2(bf16_pair(y0, y1), bf16_pair(y2, y3));
+          else
+            *(float4*)(to + 4 * e) = make_float4(y0, y1, y2, y3);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < TILES; e += 4) *(float4*)&a.part[row * HD + d0 + e] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ int splits_of(const AttendArgs& a, int T) { return max(1, (T + a.chunk - 1) / a.chunk); }
+
+// (largest logit, 1 / sum) of a query from its splits, for all lanes of the wave.
+__device__ __forceinline__ float2 joined_stats(const AttendArgs& a, int unit, int n, int n_splits, int lane) {
+  const float2* at = a.stats + (int64_t)unit * a.n_splits * a.d.N + n;
+  float top = kLowest;
+  for (int s = lane; s < n_splits; s += 64) top = fmaxf(top, at[(int64_t)s * a.d.N].x);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  float sum = 0.f;
+  for (int s = lane; s < n_splits; s += 64) {
+    const float2 x = at[(int64_t)s * a.d.N];
+    sum = fmaf(power_of_two(x.x - top), x.y, sum);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  return make_float2(top, sum);
+}
+
+// Joins the splits: one wave per query.
+template <bool BF16, int HD>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+  const int unit = blockIdx.y, lane = threadIdx.x & 63, n = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (n >= a.d.N) return;
+  int l, b, h;
+  unit_coords(a.d, unit, l, b, h);
+  const int splits = splits_of(a, seq_len(a.d, a.seq_lens, b));
+  const float2 st = joined_stats(a, unit, n, splits, lane);
+  constexpr int PER = HD / 64;
+  float x[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) x[e] = 0.f;
+  for (int s = 0; s < splits; ++s) {
+    const int64_t row = ((int64_t)unit * a.n_splits + s) * a.d.N + n;
+    const float f = power_of_two(a.stats[row].x - st.x);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) x[e] = fmaf(f, a.part[row * HD + lane * PER + e], x[e]);
+  }
+  const float inverse = st.y == 0.f ? 0.f : 1.f / st.y;
+  const int64_t at = ((int64_t)unit * a.d.N + n) * HD + lane * PER;
+  if constexpr (!BF16) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) ((float*)a.out)[at + e] = x[e] * inverse;
+  } else if constexpr (PER == 2) {
+    *(uint32_t*)(a.out + at * 2) = bf16_pair(x[0] * inverse, x[1] * inverse);
+  } else {
+    *(uint16_t*)(a.out + at * 2) = (uint16_t)bf16_pair(x[0] * inverse, 0.f);
+  }
+  if (lane == 0 && a.lse) a.lse[(int64_t)unit * a.d.N + n] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * kLn2;
+}
+
+constexpr int kWeightKeys = kThreads;  // positions per workgroup of the two kernels below
+
+// weights from stashed logits (at most 16 queries).
+__global__ __launch_bounds__(kThreads) void attend_stash_kernel(AttendArgs a) {
+  __shared__ float2 stat[16];
+  const int unit = blockIdx.y, lane = threadIdx.x & 63, N = a.d.N;
+  int l, b, h;
+  unit_coords(a.d, unit, l, b, h);
+  const int T = seq_len(a.d, a.seq_lens, b);
+  if (blockIdx.x * kWeightKeys >= T) return;
+  const int splits = splits_of(a, T);
+  for (int n = threadIdx.x >> 6; n < N; n += kWaves) {
+    const float2 st = joined_stats(a, unit, n, splits, lane);
+    if (lane == 0) stat[n] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
+  }
+  __syncthreads();
+  const int t = blockIdx.x * kWeightKeys + threadIdx.x;
+  if (t >= T) return;
+  const float* x = a.stash + (((int64_t)unit * ((a.d.t_max + 15) / 16) + t / 16) * N) * 16 + t % 16;
+  float w = 0.f;
+  for (int n = 0; n < N; ++n) w = fmaf(power_of_two(x[n * 16] - stat[n].x), stat[n].y, w);
+  const int64_t at = (int64_t)unit * a.d.t_stride + t;
+  a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + w;
+}
+
+// weights from K again: a wave takes 64 positions, 64 queries at a time.
+template <int EL, bool BF16, int HD>
+__global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a) {
+  constexpr int R = 4, STEPS = HD / 32, TERMS = BF16 ? 1 : 3, BLOCKS = 4;
+  __shared__ float2 stat[256];
+  const int unit = blockIdx.y, N = a.d.N;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int g = lane >> 4, c = lane & 15;
+  int l, b, h;
+  unit_coords(a.d, unit, l, b, h);
+  const int T = seq_len(a.d, a.seq_lens, b);
+  if (blockIdx.x * kWeightKeys >= T) return;
+  const int splits = splits_of(a, T);
+  for (int n = threadIdx.x >> 6; n < N; n += kWaves) {
+    const float2 st = joined_stats(a, unit, n, splits, lane);
+    if (lane == 0) stat[n] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
+  }
+  __syncthreads();
+  const int first = blockIdx.x * kWeightKeys + wave * 16 * BLOCKS;
+  if (first >= T) return;
+  const float to_log2 = kLog2E / sqrtf((float)HD);
+  KTile<HD> k[BLOCKS];
+#pragma unroll
+  for (int j = 0; j < BLOCKS; ++j) k[j].load(a.k, l, b, h, first / 16 + j, T, lane);
+  float w[BLOCKS][4];
+#pragma unroll
+  for (int j = 0; j < BLOCKS; ++j) w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0.f;
+  for (int row0 = 0; row0 < N; row0 += 16 * R) {
+    Queries<BF16, HD, R> q;
+    q.load(a.q + (int64_t)unit * N * HD * (BF16 ? 2 : 4), row0, N, lane);
+#pragma unroll
+    for (int j = 0; j < BLOCKS; ++j) {
+      floatx4 s[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) s[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const bf16x8 x = k[j].template operand<EL>(i);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int t = TERMS - 1; t >= 0; --t) s[r] = mma(x, q.x[r][i][t], s[r]);
+      }
+      const float scale = k[j].scale * to_log2;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int n = row0 + r * 16 + c;
+        if (n >= N) continue;
+        const float2 st = stat[n];
+        const int limit = a.causal ? T - a.d.W + 1 + n % a.d.W : T;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = power_of_two(s[r][i] * scale - st.x) * st.y;
+          if (first + 16 * j + 4 * g + i < limit) w[j][i] += p;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < BLOCKS; ++j) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) w[j][i] += __shfl_xor(w[j][i], o);
+    const int t = first + 16 * j + 4 * g + (c & 3);
+    if (c < 4 && t < T) {
+      const int64_t at = (int64_t)unit * a.d.t_stride + t;
+      const float x = c == 0 ? w[j][0] : c == 1 ? w[j][1] : c == 2 ? w[j][2] : w[j][3];
+      a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + x;
+    }
+  }
+}
+
+template <int EL, bool BF16, int HD>
+hipError_t launch(const AttendArgs& a, const AttendLayout& lay, hipStream_t s) {
+  const dim3 grid(lay.n_splits, a.d.units, lay.row_groups);
+  prof_mark("attend", s);
+  if (lay.row_tiles == 1)
+    hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 1>), grid, dim3(kThreads), 0, s, a);
+  else if (lay.row_tiles == 2)
+    hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 2>), grid, dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 4>), grid, dim3(kThreads), 0, s, a);
+  if (lay.n_splits > 1) {
+    prof_mark("attend_join", s);
+    hipLaunchKernelGGL((attend_join_kernel<BF16, HD>), dim3(div_up(a.d.N, kWaves), a.d.units), dim3(kThreads), 0, s, a);
+  }
+  if (a.weights_out) {
+    prof_mark("attend_weights", s);
+    const dim3 wgrid(div_up(a.d.t_max, kWeightKeys), a.d.units);
+    if (lay.stashed)
+      hipLaunchKernelGGL(attend_stash_kernel, wgrid, dim3(kThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL((attend_weights_kernel<EL, BF16, HD>), wgrid, dim3(kThreads), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+template <int EL, bool BF16>
+hipError_t launch_dim(const AttendArgs& a, const AttendLayout& lay, hipStream_t s) {
+  return a.d.D == 128 ? launch<EL, BF16, 128>(a, lay, s) : launch<EL, BF16, 64>(a, lay, s);
+}
+
+}  // namespace
+
+AttendLayout attend_layout(const ams_params* p) {
+  AttendLayout r;
+  const size_t units = (size_t)p->n_layers * p->batch * p->n_kv_heads, N = (size_t)p->group * p->window;
+  const int tiles = div_up(N, 16);
+  r.row_tiles = tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4;
+  r.row_groups = div_up(tiles, r.row_tiles);
+  r.stashed = N <= 16;
+  const size_t per_split = units * r.row_groups;
+  int splits = (int)max((size_t)1, (size_t)768 / per_split);
+  splits = min(splits, div_up(p->t_max, kWaves * kStep));
+  r.chunk = div_up(div_up(p->t_max, splits), kWaves * kStep) * kWaves * kStep;
+  r.n_splits = div_up(p->t_max, r.chunk);
+  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  size_t o = 0;
+  r.stats = o, o += align(units * r.n_splits * N * sizeof(float2));
+  r.part = o, o += r.n_splits > 1 ? align(units * r.n_splits * N * p->head_dim * sizeof(float)) : 0;
+  r.stash = o, o += r.stashed ? align(units * div_up(p->t_max, kBlockRows) * N * kBlockRows * sizeof(float)) : 0;
+  r.total = o;
+  return r;
+}
+
+hipError_t launch_attend(const AttendArgs& a, const AttendLayout& lay, bool bf16, int el, hipStream_t s) {
+  if (el == EL_INT8) return bf16 ? launch_dim<EL_INT8, true>(a, lay, s) : launch_dim<EL_INT8, false>(a, lay, s);
+  return bf16 ? launch_dim<EL_E4M3, true>(a, lay, s) : launch_dim<EL_E4M3, false>(a, lay, s);
+}
+
+}  // namespace ams

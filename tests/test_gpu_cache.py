@@ -1,0 +1,856 @@
+"""ams_append, ams_attend, ams_recode and ams_evict against their definitions in 64 bits, at the sizes, masks and values where they
+can go wrong, and together as a serving loop calls them.
+
+Tolerances.  Codes, scales, kept positions, counts and copied rows are exact: scales are powers of two, so every rounding is decided by
+an exact quotient, and keys that go to 8 bits are normalised and rotated in 64 bits (1e-15 against half a step of 2^-5: no
+element here lies that near the middle).  A rounding to bf16 is off by at most 2^-8 of the value, one to fp32 by 2^-24.
+attend: a logit is a sum of D exact products in fp32 on the matrix cores: at most (D / 32 + 8) roundings on the way of any product, each
+2^-24 of the sum of magnitudes A = sum_d |q_d k_d| / sqrt(D), times the scale (2 more): err_s = 16 * 2^-24 * A, plus the subtraction of
+the largest and 2^x to an ulp of its own (2^-23 each way, of |s| up to 2 A): a probability is off by err_p = 2 err_s + 2^-21 relative,
+its normalisation included.  Probabilities enter the second product with 16 bits (2^-16 with rounding of both terms), fp32: 24 (2^-23)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_23200_amd import binding as B
+from cache_util import (BLOCK, CODE, DEV, HostCache, KV, ROWS, as_code_tensor, blocks, lens_dev, loud_rows, pack_block, params, round_codes,
+                        same_bits)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- ams_recode -------------------------------------------------------------------------------------------------
+
+def _filled(kind, shape, capacity, lens, paged=False, seed=0, scale=1.0):
+    c = HostCache(kind, shape, capacity, paged, seed)
+    rng = np.random.default_rng(seed + 100)
+    for l in range(c.L):
+        for b in range(c.B):
+            for h in range(c.H):
+                for name in ("k", "v"):
+                    c.fill(name, l, b, h, loud_rows(rng, lens[b], c.D) * scale)
+    return c
+
+
+def _check_recoded(src, dst, before, n_rows, pick):
+    """dst (downloaded) against the definition; pick(l, b, h) -> source positions (-1: a row of zeros)."""
+    for l in range(src.L):
+        for b in range(src.B):
+            for h in range(src.H):
+                idx = pick(l, b, h)
+                for name in ("k", "v"):
+                    all_rows = src.rows(name, l, b, h, n_rows[b])
+                    x = np.stack([all_rows[t] if t >= 0 else np.zeros(src.D) for t in idx]) if len(idx) else np.zeros((0, src.D))
+                    for j in range(blocks(dst.capacity)):
+                        rows, at = dst.block(name, l, b, h, j)
+                        was, _ = before.block(name, l, b, h, j)
+                        part = x[j * BLOCK:(j + 1) * BLOCK]
+                        if len(part) and dst.packed:
+                            codes, scale = pack_block(part, dst.kind)
+                            np.testing.assert_equal(float(dst.t[name + "_scale"][at]), scale)
+                            same_bits(rows[:len(part)], as_code_tensor(codes, dst.kind), "codes") if scale == scale else None
+                            if not scale > 0:
+                                assert not rows[:len(part)].view(torch.uint8).any()
+                        elif len(part):
+                            same_bits(rows[:len(part)], torch.from_numpy(part).to(torch.float32).to(rows.dtype), "rows")
+                        same_bits(rows[len(part):], was[len(part):], "rows behind the last")
+
+
+KINDS = [("bf16", "int8"), ("bf16", "e4m3"), ("f32", "int8"), ("f32", "e4m3"), ("int8", "bf16"), ("e4m3", "f32"), ("int8", "f32"),
+         ("e4m3", "bf16"), ("int8", "e4m3"), ("e4m3", "int8"), ("int8", "int8"), ("e4m3", "e4m3")]
+
+
+@pytest.mark.parametrize("src_kind,dst_kind", KINDS)
+@pytest.mark.parametrize("D,paged_src,paged_dst", [(128, False, True), (64, True, False)])
+def test_recode_whole(src_kind, dst_kind, D, paged_src, paged_dst):
+    lens = [0, 1, 15, 16, 17, 70]
+    shape = (2, len(lens), 3, D)
+    src = _filled(src_kind, shape, 75, lens, paged_src, 1)
+    dst, before = HostCache(dst_kind, shape, 75, paged_dst, 2), HostCache(dst_kind, shape, 75, paged_dst, 2)
+    dtype = src_kind if src_kind in ROWS else dst_kind if dst_kind in ROWS else "bf16"
+    p = params(shape, 75, dtype=dtype)
+    B.ams_recode(p, src.upload(), lens_dev(lens), dst.upload())
+    dst.download()
+    _check_recoded(src, dst, before, lens, lambda l, b, h: list(range(lens[b])))
+
+
+@pytest.mark.parametrize("src_kind,dst_kind", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_recode_gather(src_kind, dst_kind, D):
+    """Listed rows, indices outside the cache (rows of zeros; such a row is not credited), counts of their own per unit, the credit."""
+    shape, T, budget = (1, 2, 2, D), 90, 41
+    lens = [90, 90]
+    src = _filled(src_kind, shape, T, lens, True, 3)
+    dst, before = HostCache(dst_kind, shape, budget, False, 4), HostCache(dst_kind, shape, budget, False, 4)
+    rng = np.random.default_rng(5)
+    idx = np.full((4, budget), -1, np.int32)
+    kept = np.array([41, 16, 0, 33], np.int32)
+    for u in range(4):
+        idx[u, :kept[u]] = np.sort(rng.permutation(T)[:kept[u]])
+    idx[0, 7], idx[3, 20] = T, -5
+    dtype = src_kind if src_kind in ROWS else dst_kind if dst_kind in ROWS else "bf16"
+    p = params(shape, T, dtype=dtype, budget=budget, t_stride=100)
+    credit = torch.rand((4, 100))
+    to = torch.full((4, budget), -3.0, device=DEV)
+    B.ams_recode(p, src.upload(), None, dst.upload(), torch.from_numpy(idx).to(DEV), torch.from_numpy(kept).to(DEV), credit.to(DEV), to)
+    dst.download()
+    pick = lambda l, b, h: [int(t) if 0 <= t < T else -1 for t in idx[2 * b + h, :kept[2 * b + h]]]
+    _check_recoded(src, dst, before, lens, pick)
+    for u in range(4):
+        for j in range(budget):
+            t = idx[u, j]
+            want = float(credit[u, t]) if j < kept[u] and 0 <= t < T else -3.0
+            assert float(to[u, j]) == want
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_recode_values_at_the_edges(kind):
+    """Blocks of zeros, of the smallest and largest numbers, at the border of a scale, halfway between two codes, infinite, no number."""
+    most = 127.0 if kind == "int8" else 448.0
+    x = np.zeros((16 * 12, 64), np.float32)
+    x[16] = 1e-44                                       # subnormal: scale 2^-120, codes 0
+    x[32] = 3.3e38
+    x[48:64] = -most                                    # exactly the largest code
+    x[64:80] = np.nextafter(np.float32(most), np.float32(1e9))
+    x[80, :] = np.arange(64) + 0.5                      # halfway, ties to even
+    x[80, 0] = most
+    x[96, 5], x[112, 6], x[128, 7] = np.inf, np.nan, -np.inf
+    x[144] = np.linspace(-1, 1, 64) * 2.0 ** -119       # codes under the least scale
+    x[160] = 2.0 ** np.linspace(-20, 8, 64)             # the subnormal codes of e4m3 among them
+    x[176] = np.random.default_rng(0).standard_normal(64) * 1e-3
+    shape = (1, 1, 1, 64)
+    src, dst = HostCache("f32", shape, len(x)), HostCache(kind, shape, len(x))
+    src.t["k"][0, 0, 0], src.t["v"][0, 0, 0] = torch.from_numpy(x), torch.from_numpy(-x)
+    before = HostCache(kind, shape, len(x))
+    B.ams_recode(params(shape, len(x), dtype="f32"), src.upload(), lens_dev([len(x)]), dst.upload())
+    dst.download()
+    _check_recoded(src, dst, before, [len(x)], lambda l, b, h: list(range(len(x))))
+    for j in (6, 7, 8):
+        assert math.isnan(float(dst.t["k_scale"][0, 0, 0, j])) and not dst.t["k"][0, 0, 0, 16 * j:16 * j + 16].view(torch.uint8).any()
+    assert float(dst.t["k_scale"][0, 0, 0, 0]) == 0.0 and float(dst.t["k_scale"][0, 0, 0, 1]) == 2.0 ** -120
+    assert float(dst.t["k_scale"][0, 0, 0, 3]) == 1.0 and float(dst.t["k_scale"][0, 0, 0, 4]) == 2.0
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_every_code_is_read_as_its_value(kind):
+    shape = (1, 1, 1, 64)
+    src = HostCache(kind, shape, 16)
+    src.t["k"][0, 0, 0] = torch.arange(1024).remainder(256).to(torch.uint8).view(CODE[kind]).reshape(16, 64)
+    src.t["v"].copy_(src.t["k"])
+    src.t["k_scale"].fill_(0.75)
+    src.t["v_scale"].fill_(2.0 ** 30)
+    dst = HostCache("f32", shape, 16)
+    B.ams_recode(params(shape, 16, dtype="f32"), src.upload(), lens_dev([16]), dst.upload())
+    dst.download()
+    for name, s in (("k", 0.75), ("v", 2.0 ** 30)):
+        want = src.t[name].to(torch.float32) * s
+        assert torch.equal(torch.isnan(dst.t[name]), torch.isnan(want))
+        assert torch.equal(dst.t[name].nan_to_num(), want.nan_to_num())
+
+
+def test_a_bad_table_entry_is_never_written_through():
+    shape = (1, 1, 2, 64)
+    for kind in ("int8", "bf16"):
+        src = _filled("bf16" if kind == "int8" else "e4m3", shape, 48, [48], False, 1)
+        dst = HostCache(kind, shape, 48, True, 2)
+        good = dst.table.copy()
+        for bad in (-1, 1 << 30):
+            dst.table[0, 1] = bad
+            view = dst.upload()
+            had = {k: v.clone() for k, v in dst.dev.items()}
+            B.ams_recode(params(shape, 48), src.upload(), lens_dev([48]), view)
+            mine = set((np.delete(good[0], 1)[:, None] * BLOCK + np.arange(BLOCK)).reshape(-1).tolist())
+            others = [r for r in range(dst.t["k"].shape[1]) if r not in mine]
+            for name in ("k", "v"):
+                same_bits(dst.dev[name][:, others], had[name][:, others])
+                assert not torch.equal(dst.dev[name][:, sorted(mine)].view(torch.uint8), had[name][:, sorted(mine)].view(torch.uint8))
+        dst.table[:] = good
+
+
+# ---- ams_append -------------------------------------------------------------------------------------------------
+
+def _turned(x, weight, eps, pos, rope_kw, freq):
+    """x [.., D] float64 of one token -> normalised and rotated."""
+    x = x.copy()
+    D = x.shape[-1]
+    if weight is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * weight
+    n = rope_kw["rot_dim"] if rope_kw else 0
+    if n == 0:
+        return x
+    a = (slice(0, n // 2), slice(n // 2, n)) if rope_kw["layout"] == B.ROPE_HALF else (slice(0, n, 2), slice(1, n, 2))
+    angle = pos * np.array(freq[:n // 2])
+    c, s = np.cos(angle) * rope_kw["gain"], np.sin(angle) * rope_kw["gain"]
+    y = x.copy()
+    y[..., a[0]] = x[..., a[0]] * c - x[..., a[1]] * s
+    y[..., a[1]] = x[..., a[1]] * c + x[..., a[0]] * s
+    return y
+
+
+def _append_case(kind, dtype, shape, group, lens, n_new, t_max, paged, rope_kw, norm, first, with_q=True, seed=0, fused=True, src=None):
+    """Runs one call and checks all that it writes; returns the cache (downloaded)."""
+    L, Bt, H, D = shape
+    cache = src or _filled(kind, shape, t_max, lens, paged, seed)
+    before = {k: v.clone() for k, v in cache.t.items()}
+    old_rows = {n: {} for n in ("k", "v")}
+    rng = np.random.default_rng(seed + 7)
+    heads = (group + 2) * H
+    pad = 16 if fused else 0                            # a projection's row may be longer than its heads
+    qkv = torch.from_numpy(rng.standard_normal((L, Bt, n_new, heads * D + pad))).to(ROWS[dtype])
+    dev = qkv.to(DEV)
+    view = dev[..., :heads * D].unflatten(-1, (heads, D))
+    q, k, v = view[..., :group * H, :], view[..., group * H:(group + 1) * H, :], view[..., (group + 1) * H:, :]
+    if not fused:
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    host = qkv.double().numpy()[..., :heads * D].reshape(L, Bt, n_new, heads, D)
+    w = {n: (torch.from_numpy(1 + 0.3 * rng.standard_normal(D)).to(ROWS[dtype]) if norm else None) for n in "qk"}
+    rope = B.make_rope(base=1e4, **rope_kw) if rope_kw else None
+    freq = list(rope.freq) if rope else []
+    p = params(shape, t_max, group=group, dtype=dtype)
+    q_out = torch.full((L, Bt, H * group, n_new, D), -7.0, dtype=ROWS[dtype], device=DEV)
+    lens_out = torch.full((Bt,), -9, dtype=torch.int32, device=DEV)
+    positions = torch.tensor(first, dtype=torch.int32, device=DEV) if first is not None else None
+    to_dev = lambda t: t.to(DEV) if t is not None else None
+    B.ams_append(p, q if with_q else None, k, v, to_dev(w["q"]), to_dev(w["k"]), 1e-6, rope, positions, lens_dev(lens),
+                 q_out if with_q else None, cache.upload(), lens_out)
+    assert lens_out.tolist() == [min(n + n_new, t_max) for n in lens]
+    cache.download()
+    wd = {n: t.double().numpy() if t is not None else None for n, t in w.items()}
+    got_q = q_out.double().cpu().numpy()
+    half, gain = (2.0 ** -8, abs(rope_kw["gain"]) if rope_kw else 1.0)
+    touched = set()
+    for l in range(L):
+        for b in range(Bt):
+            pos0 = first[b] if first is not None else lens[b]
+            rows = {"k": np.zeros((H, n_new, D)), "v": host[l, b, :, (group + 1) * H:].transpose(1, 0, 2)}
+            for t in range(n_new):
+                x = host[l, b, t]
+                if with_q:
+                    want = _turned(x[:group * H], wd["q"], 1e-6, pos0 + t, rope_kw, freq)
+                    # fp32 norm (10 roundings), cosine and products (4) of a pair of magnitude |x|, then one rounding to the type
+                    size = np.abs(want).max(-1, keepdims=True) * 2 + 1e-30
+                    bound = (half if dtype == "bf16" else 2.0 ** -24) * np.abs(want) + 16 * 2.0 ** -24 * size * gain
+                    assert (np.abs(got_q[l, b, :, t] - want) <= bound).all()
+                rows["k"][:, t] = _turned(x[group * H:(group + 1) * H], wd["k"], 1e-6, pos0 + t, rope_kw, freq)
+            hi = min(lens[b] + n_new, t_max)
+            for h in range(H):
+                for name in ("k", "v"):
+                    new = rows[name][h]
+                    for j in range(lens[b] // BLOCK, blocks(hi) if hi > lens[b] else lens[b] // BLOCK):
+                        lo, up = max(lens[b], j * BLOCK), min(hi, (j + 1) * BLOCK)
+                        part, old = new[lo - lens[b]:up - lens[b]], lo - j * BLOCK
+                        got, at = cache.block(name, l, b, h, j)
+                        touched.add((name, l, b, h, j))
+                        was = HostCache.block.__get__(_At(cache, before))(name, l, b, h, j)[0]
+                        if not cache.packed:
+                            size = np.abs(part).max() * 2 + 1e-30
+                            bound = (half if dtype == "bf16" else 2.0 ** -24) * np.abs(part) + (16 * 2.0 ** -24 * size * gain if name == "k" else 0)
+                            assert (np.abs(got[old:old + len(part)].double().numpy() - part) <= bound).all()
+                            same_bits(got[:old], was[:old])
+                        else:
+                            had = float(before[name + "_scale"][at]) if old else 0.0
+                            codes, scale = pack_block(part, cache.kind, had)
+                            np.testing.assert_equal(float(cache.t[name + "_scale"][at]), scale)
+                            same_bits(got[old:old + len(part)], as_code_tensor(codes, cache.kind), f"new {name} codes")
+                            if old and scale > had:
+                                again = round_codes(was[:old].float().double().numpy() * (had / scale), cache.kind)
+                                same_bits(got[:old], as_code_tensor(again, cache.kind), "old codes")
+                            else:
+                                same_bits(got[:old], was[:old])
+                        same_bits(got[old + len(part):], was[old + len(part):], "rows behind the last")
+    # every block that no new row falls into is as it was
+    for l in range(L):
+        for b in range(Bt):
+            for h in range(H):
+                for name in ("k", "v"):
+                    for j in range(blocks(t_max)):
+                        if (name, l, b, h, j) not in touched:
+                            same_bits(cache.block(name, l, b, h, j)[0], HostCache.block.__get__(_At(cache, before))(name, l, b, h, j)[0])
+    return cache
+
+
+class _At:
+    """A cache's geometry over other tensors."""
+
+    def __init__(self, cache, tensors):
+        self.__dict__.update(cache.__dict__)
+        self.t = tensors
+
+
+FULL = dict(rot_dim=128, layout=B.ROPE_HALF, gain=1.0)
+
+
+@pytest.mark.parametrize("kind,dtype", [("bf16", "bf16"), ("f32", "f32"), ("int8", "bf16"), ("e4m3", "bf16"), ("int8", "f32"), ("e4m3", "f32")])
+@pytest.mark.parametrize("n_new,paged", [(1, False), (1, True), (2, True), (37, False)])
+def test_append_types_and_lengths(kind, dtype, n_new, paged):
+    """Lengths at the edges of a block, a full sequence (nothing is written), one that the new rows overflow."""
+    lens, t_max = [0, 1, 15, 16, 31, 79, 80], 80
+    _append_case(kind, dtype, (1, len(lens), 2, 128), 2, lens, n_new, t_max, paged, FULL, True, [0, 5, 100, 70000, 1000003, 7, 9])
+
+
+@pytest.mark.parametrize("layout", [B.ROPE_HALF, B.ROPE_INTERLEAVED])
+@pytest.mark.parametrize("D,rot", [(128, 128), (128, 64), (128, 2), (128, 6), (128, 90), (64, 64), (64, 10), (64, 0)])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_append_layouts(layout, D, rot, kind):
+    _append_case(kind, "bf16", (2, 2, 3, D), 3, [5, 60], 19, 100, False, dict(rot_dim=rot, layout=layout, gain=1.3), True, [123456, 0])
+
+
+@pytest.mark.parametrize("norm,with_q,fused,rope", [(False, True, True, FULL), (True, False, True, FULL), (True, True, False, None),
+                                                   (False, False, False, None)])
+def test_append_without_its_parts(norm, with_q, fused, rope):
+    for kind in ("bf16", "int8"):
+        for n_new, layers in ((1, 1), (1, 3), (5, 2)):
+            _append_case(kind, "bf16", (layers, 2, 2, 128), 4, [40, 3], n_new, 64, False, rope, norm, None, with_q, fused=fused)
+
+
+@pytest.mark.parametrize("heads,group,n_new", [(1, 1, 1), (8, 8, 1), (8, 4, 300)])
+def test_append_many_heads_and_tokens(heads, group, n_new):
+    _append_case("int8", "bf16", (1, 1, heads, 128), group, [70], n_new, 400, True, FULL, True, None)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_append_token_by_token_grows_the_scale(kind):
+    """Sixteen calls into one block whose rows get louder: after each the codes follow the rule, and in the end no value is off by a whole
+    step of the final scale (e4m3: the steps of its floating codes, half of one each time they are rounded)."""
+    shape, t_max = (1, 1, 1, 64), 32
+    rng = np.random.default_rng(1)
+    cache = HostCache(kind, shape, t_max)
+    x = rng.standard_normal((16, 64)) * 1.6 ** np.arange(16)[:, None]
+    x = torch.from_numpy(x).to(torch.bfloat16)
+    p = params(shape, t_max)
+    view, lens = cache.upload(), lens_dev([0])
+    codes, had = np.zeros((0, 64)), 0.0
+    for t in range(16):
+        row = x[t].reshape(1, 1, 1, 1, 64).to(DEV)
+        B.ams_append(p, None, row, row, None, None, 0.0, None, None, lens, None, view)
+        lens += 1
+        new, scale = pack_block(x[t:t + 1].double().numpy(), kind, had)
+        codes = np.concatenate([round_codes(codes * (had / scale), kind) if had else codes, new])
+        had = scale
+        cache.download()
+        same_bits(cache.t["k"][0, 0, 0, :t + 1], as_code_tensor(codes, kind), f"after {t + 1}")
+        assert float(cache.t["v_scale"][0, 0, 0, 0]) == scale
+    if kind == "int8":
+        assert np.abs(codes * had - x.double().numpy()).max() < had
+
+
+def test_append_no_number_and_infinite():
+    """A new value that is infinite or no number makes its block NaN and no other; the block stays so."""
+    shape = (1, 1, 2, 64)
+    cache = _filled("int8", shape, 64, [20], False, 0)
+    x = torch.ones((1, 1, 2, 2, 64), dtype=torch.bfloat16)
+    x[0, 0, 1, 1, 3] = math.inf
+    view, lens = cache.upload(), lens_dev([20])
+    scales = {n: cache.t[n + "_scale"].clone() for n in ("k", "v")}
+    y = torch.ones_like(x)
+    y[0, 0, 0, 0, 0] = math.nan
+    p = params(shape, 64)
+    B.ams_append(p, None, x.to(DEV), y.to(DEV), None, None, 0.0, None, None, lens, None, view)
+    B.ams_append(p, None, torch.ones_like(x).to(DEV), torch.ones_like(x).to(DEV), None, None, 0.0, None, None, lens + 2, None, view)
+    cache.download()
+    nan = {n: torch.isnan(cache.t[n + "_scale"][0, 0]) for n in ("k", "v")}
+    assert nan["k"].nonzero().tolist() == [[1, 1]] and nan["v"].nonzero().tolist() == [[0, 1]]
+    assert torch.equal(cache.t["k_scale"][0, 0, :, 0], scales["k"][0, 0, :, 0])
+
+
+# ---- ams_attend -------------------------------------------------------------------------------------------------
+
+def _attend_reference(q, k, v, W, causal):
+    """q [N, D], k, v [T, D] float64 -> out, lse, p [N, T], A [N] (largest sum of magnitudes of a logit)."""
+    N, D = q.shape
+    T = len(k)
+    s = q @ k.T / math.sqrt(D)
+    seen = np.ones((N, T), bool)
+    if causal:
+        newest = T - W + np.arange(N) % W
+        seen = np.arange(T)[None] <= newest[:, None]
+    A = (np.abs(q) @ np.abs(k).T / math.sqrt(D)).max(1) if T else np.zeros(N)
+    x = np.where(seen, s, -np.inf)
+    top = x.max(1, keepdims=True) if T else np.full((N, 1), -np.inf)
+    e = np.exp(x - np.where(np.isfinite(top), top, 0.0)) if T else np.zeros((N, 0))
+    total = e.sum(1, keepdims=True)
+    p = np.divide(e, total, out=np.zeros_like(e), where=total > 0)
+    with np.errstate(divide="ignore"):
+        lse = np.where(total > 0, np.log(total) + top, -np.inf)[:, 0] if T else np.full(N, -np.inf)
+    return p @ v if T else np.zeros((N, D)), lse, p, A
+
+
+def _attend_case(cache, lens, group, W, dtype="bf16", causal=False, weights="new", lse=True, t_max=None, t_stride=None, seed=0, q_scale=1.0):
+    L, Bt, H, D = cache.L, cache.B, cache.H, cache.D
+    shape = (L, Bt, H, D)
+    t_max = t_max or cache.capacity
+    rng = np.random.default_rng(seed + 3)
+    q = torch.from_numpy(rng.standard_normal((L, Bt, H * group, W, D)) * q_scale).to(ROWS[dtype])
+    p = params(shape, t_max, group=group, window=W, dtype=dtype, causal=causal, t_stride=t_stride or t_max)
+    units, stride = L * Bt * H, p.t_stride
+    out = torch.full(q.shape, 9.0, dtype=ROWS[dtype], device=DEV)
+    got_lse = torch.full(q.shape[:4], 9.0, device=DEV) if lse else None
+    w_in = torch.from_numpy(rng.random((units, stride)).astype(np.float32)) * 4
+    w_out = {"new": torch.full((units, stride), -5.0), "same": w_in.clone(), "zero": torch.full((units, stride), -5.0), None: None}[weights]
+    w_before = w_out.clone() if w_out is not None else None
+    w_out = w_out.to(DEV) if w_out is not None else None
+    given = {"new": w_in.to(DEV), "same": w_out, "zero": None, None: None}[weights]
+    ws = torch.full((B.ams_attend_workspace_bytes(p),), 255, dtype=torch.uint8, device=DEV)     # NaN wherever it is read unwritten
+    B.ams_attend(p, cache.upload(), lens_dev(lens), q.to(DEV), out, ws, got_lse, given, w_out)
+    torch.cuda.synchronize()
+    o, hq = out.double().cpu().numpy(), q.double().numpy()
+    for l in range(L):
+        for b in range(Bt):
+            T = max(0, min(lens[b], t_max))
+            for h in range(H):
+                unit = (l * Bt + b) * H + h
+                k, v = cache.rows("k", l, b, h, T), cache.rows("v", l, b, h, T)
+                want, want_lse, pr, A = _attend_reference(hq[l, b, h * group:(h + 1) * group].reshape(group * W, D), k, v, W, causal)
+                err_p = 32 * 2.0 ** -24 * A + 2.0 ** -21                                        # [N]
+                got = o[l, b, h * group:(h + 1) * group].reshape(group * W, D)
+                terms = pr @ np.abs(v) if T else np.zeros_like(want)
+                last, half = (2.0 ** -16, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -22, 2.0 ** -24)
+                bound = half * np.abs(want) + (2 * err_p[:, None] + last) * terms + 1e-37
+                assert (np.abs(got - want) <= bound).all(), (l, b, h, T, np.abs(got - want).max(), (np.abs(got - want) / bound).max())
+                if lse:
+                    x = got_lse[l, b, h * group:(h + 1) * group].reshape(-1).double().cpu().numpy()
+                    empty = ~np.isfinite(want_lse)
+                    assert (x[empty] == -np.inf).all()
+                    assert (np.abs(x - want_lse)[~empty] <= (err_p + 2.0 ** -22 * np.abs(want_lse))[~empty]).all()
+                if weights:
+                    x = w_out[unit].double().cpu().numpy()
+                    start = w_in[unit, :T].double().numpy() if weights != "zero" else np.zeros(T)
+                    more = pr.sum(0)
+                    bound = 2 * (err_p[:, None] * pr).sum(0) + 2.0 ** -22 * more + 2.0 ** -23 * (start + more) + 1e-37
+                    assert (np.abs(x[:T] - start - more) <= bound).all(), (unit, T)
+                    assert (x[T:] == w_before[unit, T:].double().numpy()).all()
+    return out, got_lse, w_out
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("group,W,causal,paged", [(1, 1, False, False), (4, 1, True, True), (2, 8, True, False), (5, 5, False, True),
+                                                 (8, 8, True, False), (7, 11, True, True), (8, 32, True, False)])
+def test_attend_shapes(kind, dtype, D, group, W, causal, paged):
+    """Every row tile, the two ways to the weights; lengths at the edges of blocks, steps and chunks, shorter than the window, empty."""
+    lens = [0, 1, 15, 16, 17, 31, 33, 127, 128, 130, 257, 700]
+    cache = _filled(kind, (1, len(lens), 2, D), 701, lens, paged, 5)
+    _attend_case(cache, lens, group, W, dtype, causal, "new", t_stride=705)
+
+
+@pytest.mark.parametrize("T", [1, 511, 4100, 20003])
+@pytest.mark.parametrize("group,W", [(4, 1), (4, 9)])
+def test_attend_lengths_of_one_unit(T, group, W):
+    cache = _filled("int8", (1, 1, 1, 128), T + 5, [T], False, 6)
+    _attend_case(cache, [T], group, W, causal=True)
+
+
+@pytest.mark.parametrize("weights,lse", [("new", False), ("same", True), ("zero", True), (None, True), (None, False)])
+@pytest.mark.parametrize("W", [1, 20])
+def test_attend_outputs_that_are_left_out(weights, lse, W):
+    cache = _filled("e4m3", (2, 2, 2, 128), 300, [300, 77], False, 7)
+    _attend_case(cache, [300, 77], 2, W, weights=weights, lse=lse)
+
+
+def test_attend_lengths_outside_the_cache_are_clamped():
+    cache = _filled("int8", (1, 3, 1, 64), 100, [100, 100, 100], False, 8)
+    _attend_case(cache, [5000, -3, 100], 2, 2, causal=True)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_extreme_scales_and_logits(kind, dtype):
+    """Logits of thousands (one position takes all), blocks of V 2^60 apart, blocks of zeros, an all-zero cache."""
+    lens = [400, 400, 400, 400]
+    cache = _filled(kind, (1, 4, 1, 128), 400, lens, False, 9)
+    rng = np.random.default_rng(2)
+    cache.fill("k", 0, 0, 0, loud_rows(rng, 400, 128) * 300)
+    v = loud_rows(rng, 400, 128)
+    v[100:200] *= 2.0 ** 60
+    v[300:] *= 2.0 ** -60
+    cache.fill("v", 0, 1, 0, v)
+    k = loud_rows(rng, 400, 128)
+    k[64:128] = 0
+    v = loud_rows(rng, 400, 128)
+    v[:320] = 0
+    cache.fill("k", 0, 2, 0, k)
+    cache.fill("v", 0, 2, 0, v)
+    cache.fill("k", 0, 3, 0, np.zeros((400, 128)))
+    cache.fill("v", 0, 3, 0, np.zeros((400, 128)))
+    for W, causal in ((1, False), (12, True)):
+        _attend_case(cache, lens, 3, W, dtype, causal)
+
+
+def test_attend_small_probabilities_with_large_values():
+    """A position of probability 2^-40 with values 2^60 carries the output: a running reference of probabilities alone must not lose it."""
+    cache = _filled("int8", (1, 1, 1, 64), 256, [256], False, 1)
+    k = np.zeros((256, 64))
+    k[0:16, 0] = 127.0                                  # logits of 127 * 8 / 8
+    k[200, 0] = 127.0 - 28.0
+    v = np.ones((256, 64))
+    v[200] = 2.0 ** 60
+    cache.fill("k", 0, 0, 0, k)
+    cache.fill("v", 0, 0, 0, v)
+    q = torch.zeros((1, 1, 1, 1, 64))
+    q[..., 0] = 8.0
+    p = params((1, 1, 1, 64), 256)
+    out = torch.zeros((1, 1, 1, 1, 64), dtype=torch.bfloat16, device=DEV)
+    ws = torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+    B.ams_attend(p, cache.upload(), lens_dev([256]), q.to(torch.bfloat16).to(DEV), out, ws)
+    want, _, _, A = _attend_reference(q.double().numpy().reshape(1, 64), cache.rows("k", 0, 0, 0, 256), cache.rows("v", 0, 0, 0, 256), 1, False)
+    assert want.max() > 1e4
+    assert (np.abs(out.double().cpu().numpy().reshape(1, 64) - want) <= (2.0 ** -8 + 2.0 ** -15 + 64 * 2.0 ** -24 * A[:, None]) * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("W", [4, 24])
+def test_attend_nan_blocks(W):
+    """A NaN block makes the outputs of the queries that see one of its positions NaN, and of no others: not of queries whose window ends before
+    it, not of other heads, and not through positions behind the last one."""
+    T = 160
+    lens = [T, T]
+    cache = _filled("int8", (1, 2, 2, 64), 200, lens, False, 4)
+    first = T // BLOCK - 1                              # the block of the last 16 positions
+    cache.t["k_scale"][0, 0, 0, first] = math.nan
+    cache.t["v_scale"][0, 0, 1, first] = math.nan
+    cache.t["k_scale"][0, 1, :, T // BLOCK:] = math.nan
+    cache.t["v_scale"][0, 1, :, T // BLOCK:] = math.nan
+    shape = (1, 2, 2, 64)
+    p = params(shape, 200, group=2, window=W, causal=True)
+    q = torch.randn((1, 2, 4, W, 64)).to(torch.bfloat16)
+    out = torch.zeros_like(q, device=DEV)
+    w = torch.zeros((4, 200), device=DEV)
+    ws = torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+    B.ams_attend(p, cache.upload(), lens_dev(lens), q.to(DEV), out, ws, None, None, w)
+    nan = torch.isnan(out.float()).all(-1).cpu()[0]     # [batch, heads * group, W]
+    sees = torch.arange(W) + T - W >= first * BLOCK     # a query sees at least one position of the block
+    assert torch.equal(nan[0], sees.expand(4, W))
+    assert not torch.isnan(out.float()[0, 1]).any() and not torch.isnan(w[2:]).any()
+    assert not torch.isnan(w[1]).any()                  # values that are no number give their positions an ordinary weight
+    assert torch.isnan(w[0, first * BLOCK:T]).all()
+
+
+def test_attend_two_calls_give_the_same_bits():
+    cache = _filled("e4m3", (2, 2, 4, 128), 3000, [3000, 1234], True, 11)
+    for W in (1, 20):
+        a = _attend_case(cache, [3000, 1234], 2, W)
+        b = _attend_case(cache, [3000, 1234], 2, W)
+        for x, y in zip(a, b):
+            same_bits(x, y)
+
+
+def test_attend_pool_beyond_32_bits():
+    """Pages whose codes lie past 2^32 bytes of the pool."""
+    H, D, n_pages = 8, 128, (1 << 32) // (8 * 128 * 16) + 300
+    shape = (1, 1, H, D)
+    small = _filled("int8", shape, 100, [100], True, 12)
+    far = {}
+    shift = n_pages - small.t["k"].shape[1] // BLOCK
+    for name in ("k", "v"):
+        pool = torch.empty((1, n_pages * BLOCK, H, D), dtype=torch.int8, device=DEV)
+        pool[:, shift * BLOCK:] = small.t[name].to(DEV)
+        scale = torch.zeros((1, n_pages, H), device=DEV)
+        scale[:, shift:] = small.t[name + "_scale"].to(DEV)
+        far[name], far[name + "_scale"] = pool, scale
+    table = torch.from_numpy(small.table + shift).to(DEV).to(torch.int32).contiguous()
+    view = B.cache_view(far["k"], far["v"], far["k_scale"], far["v_scale"], block_table=table)
+    p = params(shape, 100, group=2)
+    q = torch.randn((1, 1, 2 * H, 1, D), device=DEV).to(torch.bfloat16)
+    outs = []
+    for c in (view, small.upload()):
+        out, ws = torch.zeros_like(q), torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+        w = torch.zeros((H, 100), device=DEV)
+        B.ams_attend(p, c, lens_dev([100]), q, out, ws, None, None, w)
+        outs.append((out, w))
+    same_bits(outs[0][0], outs[1][0])
+    same_bits(outs[0][1], outs[1][1])
+    row = torch.ones((1, 1, 1, H, D), dtype=torch.bfloat16, device=DEV)
+    B.ams_append(p, None, row, row, None, None, 0.0, None, None, lens_dev([99]), None, view)
+    slot = int(table[0, 6]) * BLOCK + 3
+    s = far["k_scale"][0, int(table[0, 6])]
+    assert torch.equal(far["k"][0, slot].float() * s[:, None], torch.ones((H, D), device=DEV).mul_(1 / s[:, None]).round().mul_(s[:, None]))
+
+
+# ---- ams_evict --------------------------------------------------------------------------------------------------
+
+def _kept(w, T, budget, n_sink, n_last):
+    kept = min(budget, T)
+    sinks = min(n_sink, kept)
+    last = min(n_last, kept - sinks)
+    rank = np.where(np.isnan(w[:T]), -np.inf, w[:T].astype(np.float64)) + 0.0
+    nan = np.isnan(w[:T])
+    middle = sorted(range(sinks, T - last), key=lambda t: (nan[t], -rank[t], t))[:kept - sinks - last]
+    return sorted(list(range(sinks)) + middle + list(range(T - last, T)))
+
+
+def _evict_case(src, dst, w, lens, budget, n_sink, n_last, dtype="bf16", t_stride=None):
+    shape, T = (src.L, src.B, src.H, src.D), src.capacity
+    p = params(shape, T, dtype=dtype, budget=budget, n_sink=n_sink, n_last=n_last, t_stride=w.shape[1])
+    before = HostCache(dst.kind, shape, dst.capacity, dst.paged)
+    before.t, before.table = {k: v.clone() for k, v in dst.t.items()}, dst.table
+    units = src.L * src.B * src.H
+    w_out = torch.full(w.shape, -5.0, device=DEV)
+    idx = torch.full((units, budget), -9, dtype=torch.int32, device=DEV)
+    n_kept = torch.full((units,), -9, dtype=torch.int32, device=DEV)
+    lens_out = torch.full((src.B,), -9, dtype=torch.int32, device=DEV)
+    ws = torch.zeros(B.ams_evict_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+    B.ams_evict(p, src.upload(), lens_dev(lens), torch.from_numpy(w).to(DEV), dst.upload(), w_out, idx, n_kept, ws, lens_out)
+    dst.download()
+    idx, n_kept, w_out = idx.cpu().numpy(), n_kept.cpu().numpy(), w_out.cpu().numpy()
+    chosen = {}
+    for u in range(units):
+        b = u // src.H % src.B
+        want = _kept(w[u], lens[b], budget, n_sink, n_last)
+        assert n_kept[u] == len(want) and int(lens_out[b]) == len(want)
+        assert idx[u, :len(want)].tolist() == want and (idx[u, len(want):] == -1).all()
+        np.testing.assert_array_equal(w_out[u, :len(want)].view(np.uint32), w[u, want].view(np.uint32))
+        assert (w_out[u, len(want):T] == 0).all() and (w_out[u, T:] == -5).all()
+        chosen[u] = want
+    _check_recoded(src, dst, before, lens, lambda l, b, h: chosen[(l * src.B + b) * src.H + h])
+
+
+@pytest.mark.parametrize("src_kind,dst_kind,dtype", [("int8", "int8", "bf16"), ("e4m3", "e4m3", "f32"), ("e4m3", "int8", "bf16"), ("bf16", "e4m3", "bf16"),
+                                                    ("int8", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f32", "f32", "f32")])
+@pytest.mark.parametrize("D,paged", [(128, True), (64, False)])
+def test_evict_types(src_kind, dst_kind, dtype, D, paged):
+    lens = [200, 1, 37, 0, 128]
+    shape = (2, len(lens), 2, D)
+    src = _filled(src_kind, shape, 200, lens, paged, 13)
+    dst = HostCache(dst_kind, shape, 60, not paged, 14)
+    w = np.random.default_rng(3).gamma(0.3, size=(20, 203)).astype(np.float32)
+    _evict_case(src, dst, w, lens, 60, 4, 10, dtype)
+
+
+@pytest.mark.parametrize("budget,n_sink,n_last", [(1, 0, 0), (1, 4, 4), (10, 4, 32), (32, 40, 3), (64, 0, 64), (64, 16, 32), (99, 0, 0), (100, 4, 32), (500, 4, 32)])
+def test_evict_budgets(budget, n_sink, n_last):
+    lens = [100, 64, 33, 1, 0]
+    shape = (1, 5, 1, 64)
+    src = _filled("int8", shape, 100, lens, False, 15)
+    w = np.random.default_rng(4).random((5, 100)).astype(np.float32)
+    _evict_case(src, HostCache("int8", shape, min(budget, 100), False, 16), w, lens, budget, n_sink, n_last)
+
+
+def test_evict_ties_and_odd_weights():
+    """Equal weights (lower position first), zeros of both signs, subnormal and negative ones, infinities, no numbers."""
+    T = 5000
+    shape = (1, 7, 1, 64)
+    rng = np.random.default_rng(5)
+    w = np.zeros((7, T), np.float32)
+    w[0] = 1.0
+    w[1] = rng.integers(0, 3, T)
+    w[2] = np.where(rng.random(T) < 0.5, -0.0, 0.0)
+    w[3] = rng.choice(np.array([np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-45, -1e-45, 3.4e38, -1.0], np.float32), T)
+    w[4] = np.nan
+    w[5] = rng.standard_normal(T)
+    w[6] = np.float32(1.0) + rng.integers(0, 200, T).astype(np.float32) * np.float32(2.0 ** -23)
+    src = _filled("int8", shape, T, [T] * 7, False, 17)
+    for budget in (700, 2300, 4999):
+        _evict_case(src, HostCache("int8", shape, budget, False, 18), w, [T] * 7, budget, 3, 30)
+
+
+@pytest.mark.parametrize("T", [1023, 1025, 9001, 40000])
+def test_evict_long_rows(T):
+    shape = (1, 2, 1, 64)
+    lens = [T, T - 700]
+    src = _filled("e4m3", shape, T, lens, True, 19)
+    w = np.exp(2 * np.random.default_rng(6).standard_normal((2, T + 3))).astype(np.float32)
+    _evict_case(src, HostCache("e4m3", shape, T // 8, False, 20), w, lens, T // 8, 4, 32)
+
+
+# ---- together ---------------------------------------------------------------------------------------------------
+
+def _loop_state(kind, steps, seed=0, paged=False):
+    """A cache bounded by a compression event, taken to 8 bits, and what a decoding loop keeps."""
+    L, Bt, H, G, D, T, budget, cap = 2, 2, 2, 3, 128, 600, 100, 128
+    rng = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=rng).to(torch.bfloat16).to(DEV)
+    s = dict(L=L, Bt=Bt, H=H, G=G, D=D, budget=budget, cap=cap, kind=kind)
+    s["K"], s["V"], s["Q"] = r(L, Bt, H, T, D), r(L, Bt, H, T, D), r(L, Bt, H * G, 8, D)
+    s["tokens"] = [r(L, Bt, 1, (G + 2) * H, D) for _ in range(steps)]
+    s["weight"] = (1 + 0.1 * r(D).float()).to(torch.bfloat16)
+    s["event"] = B.make_params(n_layers=L, batch=Bt, n_kv_heads=H, group=G, window=8, t_max=T, budget=budget, n_segments=4)
+    s["p"] = params((L, Bt, H, D), cap, group=G)
+    s["p_evict"] = params((L, Bt, H, D), cap, group=G, budget=budget, n_sink=4, n_last=16)
+    s["p_pack"] = params((L, Bt, H, D), budget, group=G)
+    units = L * Bt * H
+    z = lambda *sh, **kw: torch.zeros(sh, device=DEV, **kw)
+    s["lens_T"] = lens_dev([T] * Bt)
+    s["kd"], s["vd"] = z(L, Bt, H, budget, D, dtype=torch.bfloat16), z(L, Bt, H, budget, D, dtype=torch.bfloat16)
+    s["credit"], s["idx"], s["n_kept"] = z(units, T), z(units, budget, dtype=torch.int32), z(units, dtype=torch.int32)
+    s["ws_event"] = z(B.ams_workspace_bytes(s["event"]), dtype=torch.uint8)
+    s["side"] = []
+    for _ in range(2):                                  # the loop's cache and the one that an eviction writes
+        side = {n: z(L, Bt, H, cap, D, dtype=torch.uint8).view(CODE[kind]) for n in ("k", "v")}
+        side.update({n + "_scale": z(L, Bt, H, cap // BLOCK) for n in ("k", "v")})
+        side["w"] = z(units, cap)
+        s["side"].append(side)
+    s["ws"] = z(B.ams_attend_workspace_bytes(s["p"]), dtype=torch.uint8)
+    s["ws_evict"] = z(B.ams_evict_workspace_bytes(s["p_evict"]), dtype=torch.uint8)
+    s["q"], s["out"], s["lse"] = r(L, Bt, H * G, 1, D), z(steps, L, Bt, H * G, 1, D, dtype=torch.bfloat16), z(L, Bt, H * G, 1)
+    s["lens"] = [z(Bt, dtype=torch.int32) for _ in range(2)]
+    s["pos"] = z(Bt, dtype=torch.int32)
+    s["rope"] = B.make_rope(D)
+    return s
+
+
+def _loop(s, steps):
+    """Event -> 8 bits -> (append, attend) per token, an eviction whenever the cache is full."""
+    side, lens = 0, 0
+    B.ams_compress_step(s["event"], B.dense_view(s["K"], s["V"]), s["lens_T"], s["Q"], s["credit"], B.dense_view(s["kd"], s["vd"]), None,
+                        s["idx"], s["n_kept"], s["ws_event"])
+    view = lambda i: B.cache_view(s["side"][i]["k"], s["side"][i]["v"], s["side"][i]["k_scale"], s["side"][i]["v_scale"])
+    s["lens"][0].fill_(s["budget"])
+    s["pos"].fill_(600)
+    s["side"][0]["w"].zero_()
+    B.ams_recode(s["p_pack"], B.cache_view(s["kd"], s["vd"]), s["lens"][0], view(0))
+    G, H = s["G"], s["H"]
+    filled = s["budget"]
+    for t in range(steps):
+        if filled == s["cap"]:
+            B.ams_evict(s["p_evict"], view(side), s["lens"][lens], s["side"][side]["w"], view(1 - side), s["side"][1 - side]["w"], s["idx"],
+                        s["n_kept"], s["ws_evict"], s["lens"][1 - lens])
+            side, lens, filled = 1 - side, 1 - lens, s["budget"]
+        x = s["tokens"][t]
+        B.ams_append(s["p"], x[..., :G * H, :], x[..., G * H:(G + 1) * H, :], x[..., (G + 1) * H:, :], s["weight"], s["weight"], 1e-6, s["rope"],
+                     s["pos"], s["lens"][lens], s["q"], view(side), s["lens"][1 - lens])
+        s["pos"].add_(1)
+        lens, filled = 1 - lens, filled + 1
+        w = s["side"][side]["w"]
+        B.ams_attend(s["p"], view(side), s["lens"][lens], s["q"], s["out"][t], s["ws"], s["lse"], w, w)
+    return side
+
+
+def _host_loop(s, steps):
+    """The same loop in 64 bits from the event's kept rows on: outputs and the last weights."""
+    H, G, D = s["H"], s["G"], s["D"]
+    freq = list(s["rope"].freq)
+    wt = s["weight"].double().cpu().numpy()
+    kd, vd = s["kd"].double().cpu().numpy(), s["vd"].double().cpu().numpy()
+    outs, lasts = np.zeros((steps,) + tuple(s["out"].shape[1:])), []
+    kw = dict(rot_dim=D, layout=B.ROPE_HALF, gain=1.0)
+
+    def packed(rows):
+        return [list(pack_block(rows[j:j + BLOCK], s["kind"])) for j in range(0, len(rows), BLOCK)]
+
+    for l in range(s["L"]):
+        for b in range(s["Bt"]):
+            for h in range(H):
+                c = {"k": packed(kd[l, b, h]), "v": packed(vd[l, b, h])}
+                w = np.zeros(s["budget"])
+                value = lambda n: np.concatenate([x * sc for x, sc in c[n]])
+                for t in range(steps):
+                    if len(w) == s["cap"]:
+                        keep = _kept(w, len(w), s["budget"], 4, 16)
+                        for n in ("k", "v"):
+                            c[n] = packed(value(n)[keep])
+                        w = w[keep]
+                    x = s["tokens"][t][l, b, 0].double().cpu().numpy()
+                    rows = {"k": _turned(x[G * H + h], wt, 1e-6, 600 + t, kw, freq), "v": x[(G + 1) * H + h]}
+                    for n in ("k", "v"):
+                        if len(w) % BLOCK == 0:
+                            c[n].append(list(pack_block(rows[n][None], s["kind"])))
+                        else:
+                            had, at = c[n][-1][1], c[n][-1]
+                            new, scale = pack_block(rows[n][None], s["kind"], had)
+                            old = round_codes(at[0] * (had / scale), s["kind"]) if scale > had else at[0]
+                            at[0], at[1] = np.concatenate([old, new]), scale
+                    q = _turned(x[h * G:(h + 1) * G], wt, 1e-6, 600 + t, kw, freq)
+                    q = torch.from_numpy(q).to(torch.bfloat16).double().numpy()
+                    o, _, p, _ = _attend_reference(q, value("k"), value("v"), 1, False)
+                    outs[t, l, b, h * G:(h + 1) * G, 0] = o
+                    w = np.append(w, 0.0) + p.sum(0)
+                lasts.append(w)
+    return outs, np.stack(lasts)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_a_decoding_loop(kind):
+    """From a compression event through two evictions.  A query that rounds to the other bf16 neighbour on the GPU moves a logit by up to
+    2^-8 of one product (|q k| / sqrt(D) < 8 here): outputs are held to 2^-8 of themselves plus 2^-5 of the largest, weights to 2^-5; a different kept
+    position or code would show as a difference of the order of the values themselves."""
+    steps = 70
+    s = _loop_state(kind, steps)
+    side = _loop(s, steps)
+    want, weights = _host_loop(s, steps)
+    got = s["out"].double().cpu().numpy()
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -5 * np.abs(want).max()).all()
+    assert np.linalg.norm(got - want) <= 2.0 ** -7 * np.linalg.norm(want)
+    n = weights.shape[1]
+    w = s["side"][side]["w"].double().cpu().numpy()
+    assert (np.abs(w[:, :n] - weights) <= 2.0 ** -5 * (1 + weights)).all() and (w[:, n:] == 0).all()
+
+
+def test_a_captured_loop_replays():
+    """The loop in one graph, replayed with other work between: every replay gives the eager bits."""
+    steps = 40
+    s = _loop_state("int8", steps, seed=5)
+    _loop(s, steps)
+    torch.cuda.synchronize()
+    want = [s["out"].clone(), s["side"][0]["w"].clone(), s["side"][1]["w"].clone(), s["side"][1]["k"].clone()]
+    # the first run on the capturing stream happens before the capture
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        s["credit"].zero_()
+        _loop(s, steps)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        s["credit"].zero_()
+        _loop(s, steps)
+    for i in range(4):
+        s["out"].fill_(3.0)
+        s["side"][i % 2]["w"].fill_(1e9)
+        torch.randn(1000, device=DEV).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, (s["out"], s["side"][0]["w"], s["side"][1]["w"], s["side"][1]["k"])):
+            same_bits(a, b, f"replay {i}")
+
+
+def test_two_streams_at_once():
+    """Two calls in flight on streams of their own, each with its workspace."""
+    cache = _filled("int8", (1, 4, 4, 128), 4000, [4000] * 4, False, 21)
+    view, lens = cache.upload(), lens_dev([4000] * 4)
+    p = params((1, 4, 4, 128), 4000, group=4)
+    jobs = []
+    for i in range(2):
+        q = torch.randn((1, 4, 16, 1, 128), device=DEV).to(torch.bfloat16)
+        jobs.append(dict(q=q, out=torch.zeros_like(q), w=torch.zeros((16, 4000), device=DEV), stream=torch.cuda.Stream(),
+                         ws=torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)))
+    alone = []
+    for j in jobs:
+        B.ams_attend(p, view, lens, j["q"], j["out"], j["ws"], None, None, j["w"])
+        alone.append((j["out"].clone(), j["w"].clone()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for j in jobs:
+            with torch.cuda.stream(j["stream"]):
+                B.ams_attend(p, view, lens, j["q"], j["out"], j["ws"], None, None, j["w"])
+    torch.cuda.synchronize()
+    for j, (out, w) in zip(jobs, alone):
+        same_bits(j["out"], out)
+        same_bits(j["w"], w)
+
+
+def test_binding_refusals():
+    cache = _filled("int8", (1, 1, 2, 64), 40, [40], False, 22)
+    view = cache.upload()
+    p = params((1, 1, 2, 64), 40, group=2)
+    q = torch.zeros((1, 1, 4, 1, 64), dtype=torch.bfloat16, device=DEV)
+    ws = torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+    lens = lens_dev([40])
+    good = dict(p=p, src=view, seq_lens=lens, q=q, out=torch.zeros_like(q), ws=ws)
+    for bad in (dict(q=q.cpu()), dict(q=q.float()), dict(out=q[..., :32]), dict(seq_lens=lens.long()), dict(seq_lens=lens.cpu()),
+                dict(lse=torch.zeros(3, device=DEV)), dict(weights_out=torch.zeros(70, device=DEV)), dict(ws=ws.float()),
+                dict(p=params((1, 1, 2, 128), 40, group=2)), dict(p=params((1, 2, 2, 64), 40, group=2))):
+        with pytest.raises(ValueError):
+            B.ams_attend(**dict(good, **bad))
+    with pytest.raises(B.AmsError) as e:
+        B.ams_attend(**dict(good, ws=ws[:16]))
+    assert e.value.status == B.ERR_WORKSPACE_TOO_SMALL
+    row = torch.zeros((1, 1, 1, 2, 64), dtype=torch.bfloat16, device=DEV)
+    wide = torch.zeros((1, 1, 1, 2, 128), dtype=torch.bfloat16, device=DEV)
+    for k in (row.cpu(), row.float(), row[..., :32], wide[..., ::2], row[:, :, :, :1]):
+        with pytest.raises(ValueError):
+            B.ams_append(p, None, k, row, None, None, 0.0, None, None, lens, None, view)
+    t = cache.dev
+    for args in ((t["k"], t["v"]), (t["k"], t["v"], t["k_scale"], t["v_scale"][..., :2].contiguous()), (t["k"], t["v"].float(), t["k_scale"], t["v_scale"]),
+                 (t["k"], t["v"][..., ::2], t["k_scale"], t["v_scale"]), (t["k"][0], t["v"][0], t["k_scale"], t["v_scale"])):
+        with pytest.raises(ValueError):
+            B.cache_view(*args)
