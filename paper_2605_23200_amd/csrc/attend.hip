@@ -117,19 +117,70 @@ struct Queries {
   }
 };
 
+// Loads of what no kernel here writes and every lane of the wave wants: through the scalar cache.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
+// The blocks of one unit: slot of a block (the block itself, or its page), bytes and scales from slot to slot, the same for K and V.
+struct UnitBlocks {
+  const char *k, *v;
+  const float *k_scale, *v_scale;
+  const int32_t* table;  // null: dense
+  int64_t block_bytes, scale_step, n_pages;
+  int row_stride;
+  __device__ __forceinline__ UnitBlocks(const CacheDev& kc, const CacheDev& vc, int l, int b, int h) {
+    const Block k0 = first(kc, l, b, h), v0 = first(vc, l, b, h);
+    k = k0.row0, v = v0.row0, k_scale = kc.scale + k0.scale, v_scale = vc.scale + v0.scale;
+    table = kc.paged ? kc.table + (int64_t)b * kc.max_blocks : nullptr;
+    row_stride = (int)k0.stride;
+    block_bytes = k0.stride * kBlockRows;
+    scale_step = kc.paged ? kc.H : 1;
+    n_pages = kc.n_pages;
+  }
+  static __device__ __forceinline__ Block first(const CacheDev& c, int l, int b, int h) {
+    Block r;
+    const int64_t unit = ((int64_t)l * c.B + b) * c.H + h;
+    r.row0 = c.base + (c.paged ? (int64_t)l * c.n_slots * c.H + h : unit * c.t_capacity) * c.row_bytes;
+    r.stride = c.paged ? (int64_t)c.H * c.row_bytes : c.row_bytes;
+    r.scale = c.paged ? (int64_t)l * c.n_pages * c.H + h : unit * ((c.t_capacity + kBlockRows - 1) / kBlockRows);
+    r.there = true;
+    return r;
+  }
+  __device__ __forceinline__ int64_t slot(int blk) const {
+    if (!table) return blk;
+    const int64_t page = uniform_load(table + blk);
+    return page < 0 ? 0 : page < n_pages ? page : n_pages - 1;
+  }
+};
+
+// A lane's byte offsets in two blocks: row lane % 16 of K, rows 4 (lane / 16) + 0..3 of V.  Rows past the last position (of the
+// sequence's last blocks) are that position again: what is behind it, in the cache or past its end, is not read.
+template <int HD>
+struct Offsets {
+  uint32_t k[2], v[2][4];
+  __device__ __forceinline__ void set(int row_stride, int lane, int most0, int most1) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int most = j ? most1 : most0;
+      k[j] = (uint32_t)min(lane & 15, most) * row_stride + (lane >> 4) * 16;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[j][i] = (uint32_t)min((lane >> 4) * 4 + i, most) * row_stride + (lane & 15) * (HD / 16);
+    }
+  }
+};
+
 // A block of K as the wave reads it: lane % 16 is the position, lane / 16 the 16 bytes of every 64.
 template <int HD>
 struct KTile {
   uint4 w[HD / 64];
   float scale;
-  // rows past the last one read that one again; a block past the last one likewise
-  __device__ __forceinline__ void load(const CacheDev& c, int l, int b, int h, int blk, int T, int lane) {
-    const int use = min(blk, (T - 1) / kBlockRows);
-    const Block k = block_at(c, l, b, h, use);
-    scale = c.scale[k.scale];
-    const char* row = k.row0 + min(lane & 15, T - 1 - use * kBlockRows) * k.stride + (lane >> 4) * 16;
+  __device__ __forceinline__ void load(const UnitBlocks& u, int64_t slot, uint32_t offset) {
+    scale = uniform_load(u.k_scale + slot * u.scale_step);
+    const char* row = u.k + slot * u.block_bytes;
 #pragma unroll
-    for (int i = 0; i < HD / 64; ++i) w[i] = *(const uint4*)(row + 64 * i);
+    for (int i = 0; i < HD / 64; ++i) w[i] = *(const uint4*)(row + offset + 64 * i);
   }
   template <int EL>
   __device__ __forceinline__ bf16x8 operand(int i) const {
@@ -143,20 +194,19 @@ struct VTile {
   static constexpr int WORDS = HD / 64;  // of 4 channels
   uint32_t w[WORDS][8];
   float scale[2];
-  __device__ __forceinline__ void load(const CacheDev& c, int l, int b, int h, int blk, int T, int lane) {
+  __device__ __forceinline__ void load(const UnitBlocks& u, int64_t slot0, int64_t slot1, const Offsets<HD>& o) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int use = min(blk + j, (T - 1) / kBlockRows);
-      const Block v = block_at(c, l, b, h, use);
-      scale[j] = c.scale[v.scale];
+      const int64_t slot = j ? slot1 : slot0;
+      scale[j] = uniform_load(u.v_scale + slot * u.scale_step);
+      const char* block = u.v + slot * u.block_bytes;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const char* at = v.row0 + min((lane >> 4) * 4 + i, T - 1 - use * kBlockRows) * v.stride + (lane & 15) * (HD / 16);
         if constexpr (WORDS == 2) {
-          const uint2 x = *(const uint2*)at;
+          const uint2 x = *(const uint2*)(block + o.v[j][i]);
           w[0][4 * j + i] = x.x, w[1][4 * j + i] = x.y;
         } else {
-          w[0][4 * j + i] = *(const uint32_t*)at;
+          w[0][4 * j + i] = *(const uint32_t*)(block + o.v[j][i]);
         }
       }
     }
@@ -165,7 +215,7 @@ struct VTile {
 
 // One split of one unit's positions for 16 R of its queries.
 template <int EL, bool BF16, int HD, int R>
-__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) void attend_kernel(AttendArgs a) {
   constexpr int STEPS = HD / 32, TILES = HD / 16, TERMS = BF16 ? 1 : 3, PTERMS = BF16 ? 2 : 3;
   constexpr int LD = HD + 4;  // row of the join in LDS
   __shared__ __align__(16) float joint[kWaves][16][LD];
@@ -197,21 +247,39 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     for (int e = 0; e < TILES; ++e) o[r][e] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
   const float to_log2 = kLog2E / sqrtf((float)HD);
+  const UnitBlocks u(a.k, a.v, l, b, h);
+  const int last_blk = (T - 1) / kBlockRows;
+  Offsets<HD> off;
+  off.set(u.row_stride, lane, kBlockRows - 1, kBlockRows - 1);
   KTile<HD> kt[2];
   VTile<HD> vt;
+  int64_t slot[2] = {0, 0};
+  // slots of the step's two blocks; its offsets where it holds the sequence's end (the wave's last step)
+  auto find = [&](int at) __attribute__((always_inline)) {
+    slot[0] = u.slot(at / kBlockRows);
+    slot[1] = u.slot(min(at / kBlockRows + 1, last_blk));
+  };
+  auto ends = [&](int at) __attribute__((always_inline)) {
+    if (at + kStep > T) {
+      const int blk1 = min(at / kBlockRows + 1, last_blk);
+      off.set(u.row_stride, lane, min(T - 1 - at, kBlockRows - 1), T - 1 - blk1 * kBlockRows);
+    }
+  };
   int at = begin + wave * kStep;
   if (at < end) {
-    kt[0].load(a.k, l, b, h, at / kBlockRows, T, lane);
-    kt[1].load(a.k, l, b, h, at / kBlockRows + 1, T, lane);
-    vt.load(a.v, l, b, h, at / kBlockRows, T, lane);
+    find(at);
+    ends(at);
+    kt[0].load(u, slot[0], off.k[0]);
+    kt[1].load(u, slot[1], off.k[1]);
+    vt.load(u, slot[0], slot[1], off);
+    if (at + kWaves * kStep < end) find(at + kWaves * kStep);
   }
   for (; at < end; at += kWaves * kStep) {
     floatx4 s[2][R];
-    float kscale[2], vscale[2];
-    VTile<HD> v = vt;
+    float kscale[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      kscale[j] = kt[j].scale * to_log2, vscale[j] = vt.scale[j];
+      kscale[j] = kt[j].scale * to_log2;
 #pragma unroll
       for (int r = 0; r < R; ++r) s[j][r] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -225,9 +293,9 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     }
     const int next = at + kWaves * kStep;
     if (next < end) {
-      kt[0].load(a.k, l, b, h, next / kBlockRows, T, lane);
-      kt[1].load(a.k, l, b, h, next / kBlockRows + 1, T, lane);
-      vt.load(a.v, l, b, h, next / kBlockRows, T, lane);
+      ends(next);
+      kt[0].load(u, slot[0], off.k[0]);
+      kt[1].load(u, slot[1], off.k[1]);
     }
     const bool whole = at + kStep <= fewest;  // every query sees every position of the step
     bf16x8 p[R][PTERMS];
@@ -258,7 +326,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
       for (int j = 0; j < 8; j += 2) {
         float p0 = power_of_two(x[j] - m[r]), p1 = power_of_two(x[j + 1] - m[r]);
         sum[r] += p0 + p1;
-        p0 *= vscale[j >> 2], p1 *= vscale[j >> 2];
+        p0 *= vt.scale[j >> 2], p1 *= vt.scale[j >> 2];
         if (!whole) {  // a scale that is no number at a position that the query does not see
           if (x[j] == -INFINITY) p0 = 0.f;
           if (x[j + 1] == -INFINITY) p1 = 0.f;
@@ -277,14 +345,18 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
 #pragma unroll
     for (int w = 0; w < VTile<HD>::WORDS; ++w) {
       bf16x8 e[4];
-      turn_pair<EL, 0>(v.w[w], e[0], e[1]);
-      turn_pair<EL, 1>(v.w[w], e[2], e[3]);
+      turn_pair<EL, 0>(vt.w[w], e[0], e[1]);
+      turn_pair<EL, 1>(vt.w[w], e[2], e[3]);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
           for (int t = PTERMS - 1; t >= 0; --t) o[r][4 * w + k] = mma(e[k], p[r][t], o[r][4 * w + k]);
+    }
+    if (next < end) {
+      vt.load(u, slot[0], slot[1], off);
+      if (next + kWaves * kStep < end) find(next + kWaves * kStep);
     }
   }
   // the four waves together: 16 queries at a time, thread (query, stretch of HD / 16 channels)
@@ -319,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     if (n < N) {
       const int64_t row = ((int64_t)unit * a.n_splits + split) * N + n;
       if (threadIdx.x % 16 == 0) {
-        a.stats[row] = make_float2(top, all);
+        a.stats[((int64_t)unit * N + n) * a.n_splits + split] = make_float2(top, all);
         if (last && a.lse) a.lse[(int64_t)unit * N + n] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
       }
       if (last) {
@@ -343,79 +415,112 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
 
 __device__ __forceinline__ int splits_of(const AttendArgs& a, int T) { return max(1, (T + a.chunk - 1) / a.chunk); }
 
-// (largest logit, 1 / sum) of a query from its splits, for all lanes of the wave.
+// (largest logit, sum) of a query from its splits, for all lanes of the wave.
 __device__ __forceinline__ float2 joined_stats(const AttendArgs& a, int unit, int n, int n_splits, int lane) {
-  const float2* at = a.stats + (int64_t)unit * a.n_splits * a.d.N + n;
+  const float2* at = a.stats + ((int64_t)unit * a.d.N + n) * a.n_splits;
   float top = kLowest;
-  for (int s = lane; s < n_splits; s += 64) top = fmaxf(top, at[(int64_t)s * a.d.N].x);
+  for (int s = lane; s < n_splits; s += 64) top = fmaxf(top, at[s].x);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   float sum = 0.f;
-  for (int s = lane; s < n_splits; s += 64) {
-    const float2 x = at[(int64_t)s * a.d.N];
-    sum = fmaf(power_of_two(x.x - top), x.y, sum);
-  }
+  for (int s = lane; s < n_splits; s += 64) sum = fmaf(power_of_two(at[s].x - top), at[s].y, sum);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   return make_float2(top, sum);
 }
 
-// Joins the splits: one wave per query.
+// Joins the splits of query n: a wave takes every fourth split, its lanes HD / 64 channels each; then the waves together.
 template <bool BF16, int HD>
-__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
-  const int unit = blockIdx.y, lane = threadIdx.x & 63, n = blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (n >= a.d.N) return;
-  int l, b, h;
-  unit_coords(a.d, unit, l, b, h);
-  const int splits = splits_of(a, seq_len(a.d, a.seq_lens, b));
-  const float2 st = joined_stats(a, unit, n, splits, lane);
+__device__ __forceinline__ void join_splits(const AttendArgs& a, int unit, int n, int splits) {
   constexpr int PER = HD / 64;
+  __shared__ float part[kWaves][HD];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const float2 st = joined_stats(a, unit, n, splits, lane);
+  const float2* stats = a.stats + ((int64_t)unit * a.d.N + n) * a.n_splits;
   float x[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) x[e] = 0.f;
-  for (int s = 0; s < splits; ++s) {
-    const int64_t row = ((int64_t)unit * a.n_splits + s) * a.d.N + n;
-    const float f = power_of_two(a.stats[row].x - st.x);
+  const float* from = a.part + ((int64_t)unit * a.n_splits * a.d.N + n) * HD + lane * PER;
+  const int64_t step = (int64_t)a.d.N * HD;
+  for (int s0 = wave; s0 < splits; s0 += 64 * kWaves) {
+    const int mine = s0 + kWaves * lane;
+    const float f = mine < splits ? power_of_two(stats[mine].x - st.x) : 0.f;
+    const int n_here = min(64, (splits - s0 + kWaves - 1) / kWaves);
+    for (int i0 = 0; i0 < n_here; i0 += 8) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) x[e] = fmaf(f, a.part[row * HD + lane * PER + e], x[e]);
+      for (int i = 0; i < 8; ++i) {
+        const float fi = __shfl(f, i0 + i);  // 0 past the last split, which is read again
+        const float* at = from + (s0 + kWaves * min(i0 + i, n_here - 1)) * step;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] = fmaf(fi, at[e], x[e]);
+      }
+    }
   }
+#pragma unroll
+  for (int e = 0; e < PER; ++e) part[wave][lane * PER + e] = x[e];
+  __syncthreads();
+  if (wave > 0) return;
   const float inverse = st.y == 0.f ? 0.f : 1.f / st.y;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) x[e] += part[w][lane * PER + e];
+    x[e] *= inverse;
+  }
   const int64_t at = ((int64_t)unit * a.d.N + n) * HD + lane * PER;
   if constexpr (!BF16) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) ((float*)a.out)[at + e] = x[e] * inverse;
+    for (int e = 0; e < PER; ++e) ((float*)a.out)[at + e] = x[e];
   } else if constexpr (PER == 2) {
-    *(uint32_t*)(a.out + at * 2) = bf16_pair(x[0] * inverse, x[1] * inverse);
+    *(uint32_t*)(a.out + at * 2) = bf16_pair(x[0], x[1]);
   } else {
-    *(uint16_t*)(a.out + at * 2) = (uint16_t)bf16_pair(x[0] * inverse, 0.f);
+    *(uint16_t*)(a.out + at * 2) = (uint16_t)bf16_pair(x[0], 0.f);
   }
-  if (lane == 0 && a.lse) a.lse[(int64_t)unit * a.d.N + n] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * kLn2;
+  if (lane == 0) {
+    if (a.lse) a.lse[(int64_t)unit * a.d.N + n] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * kLn2;
+    if (a.joined) a.joined[(int64_t)unit * a.d.N + n] = st;
+  }
 }
 
-constexpr int kWeightKeys = kThreads;  // positions per workgroup of the two kernels below
+constexpr int kStashKeys = 4 * kThreads;  // positions per workgroup that turns stashed logits into weights
 
-// weights from stashed logits (at most 16 queries).
-__global__ __launch_bounds__(kThreads) void attend_stash_kernel(AttendArgs a) {
+// The workgroups of one unit: N of them join the splits (where there is more than one), the others form the weights from stashed logits.
+template <bool BF16, int HD>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int joins) {
   __shared__ float2 stat[16];
   const int unit = blockIdx.y, lane = threadIdx.x & 63, N = a.d.N;
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
-  const int T = seq_len(a.d, a.seq_lens, b);
-  if (blockIdx.x * kWeightKeys >= T) return;
-  const int splits = splits_of(a, T);
+  const int T = seq_len(a.d, a.seq_lens, b), splits = splits_of(a, T);
+  if ((int)blockIdx.x < joins) {
+    join_splits<BF16, HD>(a, unit, blockIdx.x, splits);
+    return;
+  }
+  const int first = ((int)blockIdx.x - joins) * kStashKeys;
+  if (first >= T) return;
   for (int n = threadIdx.x >> 6; n < N; n += kWaves) {
     const float2 st = joined_stats(a, unit, n, splits, lane);
     if (lane == 0) stat[n] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
   }
   __syncthreads();
-  const int t = blockIdx.x * kWeightKeys + threadIdx.x;
+  const int t = first + 4 * threadIdx.x;
   if (t >= T) return;
   const float* x = a.stash + (((int64_t)unit * ((a.d.t_max + 15) / 16) + t / 16) * N) * 16 + t % 16;
-  float w = 0.f;
-  for (int n = 0; n < N; ++n) w = fmaf(power_of_two(x[n * 16] - stat[n].x), stat[n].y, w);
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int n = 0; n < N; ++n) {
+    const float4 s = *(const float4*)(x + n * 16);
+    const float2 st = stat[n];
+    w[0] = fmaf(power_of_two(s.x - st.x), st.y, w[0]), w[1] = fmaf(power_of_two(s.y - st.x), st.y, w[1]);
+    w[2] = fmaf(power_of_two(s.z - st.x), st.y, w[2]), w[3] = fmaf(power_of_two(s.w - st.x), st.y, w[3]);
+  }
   const int64_t at = (int64_t)unit * a.d.t_stride + t;
-  a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (t + i < T) a.weights_out[at + i] = (a.weights_in ? a.weights_in[at + i] : 0.f) + w[i];
 }
+
+constexpr int kWeightKeys = kThreads;  // positions per workgroup of the kernel below
 
 // weights from K again: a wave takes 64 positions, 64 queries at a time.
 template <int EL, bool BF16, int HD>
@@ -429,18 +534,21 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a) 
   unit_coords(a.d, unit, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b);
   if (blockIdx.x * kWeightKeys >= T) return;
-  const int splits = splits_of(a, T);
-  for (int n = threadIdx.x >> 6; n < N; n += kWaves) {
-    const float2 st = joined_stats(a, unit, n, splits, lane);
-    if (lane == 0) stat[n] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
+  if ((int)threadIdx.x < N) {  // joined, or of the only split
+    const float2 st = a.joined[(int64_t)unit * N + threadIdx.x];
+    stat[threadIdx.x] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
   }
   __syncthreads();
   const int first = blockIdx.x * kWeightKeys + wave * 16 * BLOCKS;
   if (first >= T) return;
   const float to_log2 = kLog2E / sqrtf((float)HD);
+  const UnitBlocks u(a.k, a.v, l, b, h);
   KTile<HD> k[BLOCKS];
 #pragma unroll
-  for (int j = 0; j < BLOCKS; ++j) k[j].load(a.k, l, b, h, first / 16 + j, T, lane);
+  for (int j = 0; j < BLOCKS; ++j) {
+    const int blk = min(first / kBlockRows + j, (T - 1) / kBlockRows);
+    k[j].load(u, u.slot(blk), (uint32_t)min(lane & 15, T - 1 - blk * kBlockRows) * u.row_stride + (lane >> 4) * 16);
+  }
   float w[BLOCKS][4];
 #pragma unroll
   for (int j = 0; j < BLOCKS; ++j) w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0.f;
@@ -500,17 +608,14 @@ hipError_t launch(const AttendArgs& a, const AttendLayout& lay, hipStream_t s) {
     hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 2>), grid, dim3(kThreads), 0, s, a);
   else
     hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 4>), grid, dim3(kThreads), 0, s, a);
-  if (lay.n_splits > 1) {
+  const int joins = lay.n_splits > 1 ? a.d.N : 0, stash = a.stash ? div_up(a.d.t_max, kStashKeys) : 0;
+  if (joins + stash > 0) {
     prof_mark("attend_join", s);
-    hipLaunchKernelGGL((attend_join_kernel<BF16, HD>), dim3(div_up(a.d.N, kWaves), a.d.units), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((attend_join_kernel<BF16, HD>), dim3(joins + stash, a.d.units), dim3(kThreads), 0, s, a, joins);
   }
-  if (a.weights_out) {
+  if (a.weights_out && !a.stash) {
     prof_mark("attend_weights", s);
-    const dim3 wgrid(div_up(a.d.t_max, kWeightKeys), a.d.units);
-    if (lay.stashed)
-      hipLaunchKernelGGL(attend_stash_kernel, wgrid, dim3(kThreads), 0, s, a);
-    else
-      hipLaunchKernelGGL((attend_weights_kernel<EL, BF16, HD>), wgrid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((attend_weights_kernel<EL, BF16, HD>), dim3(div_up(a.d.t_max, kWeightKeys), a.d.units), dim3(kThreads), 0, s, a);
   }
   return hipGetLastError();
 }
@@ -529,14 +634,22 @@ AttendLayout attend_layout(const ams_params* p) {
   r.row_tiles = tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4;
   r.row_groups = div_up(tiles, r.row_tiles);
   r.stashed = N <= 16;
+  // Positions per workgroup: 512 where that fills the chip several times over (ragged sequences end at different times), else
+  // as many as give one round of workgroups, three on a CU.
   const size_t per_split = units * r.row_groups;
-  int splits = (int)max((size_t)1, (size_t)768 / per_split);
-  splits = min(splits, div_up(p->t_max, kWaves * kStep));
-  r.chunk = div_up(div_up(p->t_max, splits), kWaves * kStep) * kWaves * kStep;
+  const size_t fine = per_split * div_up(p->t_max, 512);
+  if (fine >= 2048) {
+    r.chunk = 512;
+  } else {
+    const int splits = (int)max((size_t)1, (size_t)768 / per_split);
+    r.chunk = div_up(div_up(p->t_max, splits), kWaves * kStep) * kWaves * kStep;
+  }
+  while (div_up(p->t_max, r.chunk) > 4096) r.chunk *= 2;  // what the join goes through
   r.n_splits = div_up(p->t_max, r.chunk);
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
   size_t o = 0;
   r.stats = o, o += align(units * r.n_splits * N * sizeof(float2));
+  r.joined = o, o += r.n_splits > 1 && !r.stashed ? align(units * N * sizeof(float2)) : 0;
   r.part = o, o += r.n_splits > 1 ? align(units * r.n_splits * N * p->head_dim * sizeof(float)) : 0;
   r.stash = o, o += r.stashed ? align(units * div_up(p->t_max, kBlockRows) * N * kBlockRows * sizeof(float)) : 0;
   r.total = o;

@@ -156,7 +156,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 
 // Where scratch of ams_attend lies.
 struct AttendLayout {
-  size_t part, stats, stash, total;  // outputs and statistics of the splits, logits
+  size_t part, stats, joined, stash, total;  // outputs and statistics of the splits, logits
   int chunk, n_splits, row_tiles, row_groups;
   bool stashed;  // the logits are kept for the weights
 };
@@ -187,7 +187,8 @@ struct AttendArgs {
   float* weights_out;
   int causal;
   float* part;    // [units, splits, N, D]
-  float2* stats;  // [units, splits, N]: largest logit (log2), sum
+  float2* stats;  // [units, N, splits]: largest logit (log2), sum
+  float2* joined; // [units, N], where the weights come from K again
   float* stash;   // [units, blocks, N, 16]
   int chunk, n_splits;
 };
