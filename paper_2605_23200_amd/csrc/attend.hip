@@ -148,10 +148,11 @@ struct UnitBlocks {
     r.there = true;
     return r;
   }
-  __device__ __forceinline__ int64_t slot(int blk) const {
-    if (!table) return blk;
-    const int64_t page = uniform_load(table + blk);
-    return page < 0 ? 0 : page < n_pages ? page : n_pages - 1;
+  // The table's word, and the slot that it names: apart, so that the word can be on its way for a while.
+  __device__ __forceinline__ int named(int blk) const { return table ? uniform_load(table + blk) : blk; }
+  __device__ __forceinline__ int64_t slot(int name) const {
+    if (!table) return name;
+    return name < 0 ? 0 : name < n_pages ? name : n_pages - 1;
   }
 };
 
@@ -253,28 +254,25 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) 
   off.set(u.row_stride, lane, kBlockRows - 1, kBlockRows - 1);
   KTile<HD> kt[2];
   VTile<HD> vt;
+  int name[2] = {0, 0};
   int64_t slot[2] = {0, 0};
-  // slots of the step's two blocks; its offsets where it holds the sequence's end (the wave's last step)
+  // names of the step's two blocks; its offsets where it holds the sequence's end (the wave's last step)
   auto find = [&](int at) __attribute__((always_inline)) {
-    slot[0] = u.slot(at / kBlockRows);
-    slot[1] = u.slot(min(at / kBlockRows + 1, last_blk));
+    name[0] = u.named(min(at / kBlockRows, last_blk));
+    name[1] = u.named(min(at / kBlockRows + 1, last_blk));
   };
-  auto ends = [&](int at) __attribute__((always_inline)) {
+  auto settle = [&](int at) __attribute__((always_inline)) {
+    slot[0] = u.slot(name[0]), slot[1] = u.slot(name[1]);
     if (at + kStep > T) {
       const int blk1 = min(at / kBlockRows + 1, last_blk);
       off.set(u.row_stride, lane, min(T - 1 - at, kBlockRows - 1), T - 1 - blk1 * kBlockRows);
     }
   };
   int at = begin + wave * kStep;
-  if (at < end) {
-    find(at);
-    ends(at);
-    kt[0].load(u, slot[0], off.k[0]);
-    kt[1].load(u, slot[1], off.k[1]);
-    vt.load(u, slot[0], slot[1], off);
-    if (at + kWaves * kStep < end) find(at + kWaves * kStep);
-  }
-  for (; at < end; at += kWaves * kStep) {
+  // One step.  MORE: there is another, whose K is loaded when this one's has been used, V likewise.  (Loads under a condition that
+  // the compiler cannot follow would make every wait one for all loads.)
+  auto step = [&](auto more) __attribute__((always_inline)) {
+    constexpr bool MORE = decltype(more)::value;
     floatx4 s[2][R];
     float kscale[2];
 #pragma unroll
@@ -292,10 +290,11 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) 
       }
     }
     const int next = at + kWaves * kStep;
-    if (next < end) {
-      ends(next);
+    if constexpr (MORE) {
+      settle(next);
       kt[0].load(u, slot[0], off.k[0]);
       kt[1].load(u, slot[1], off.k[1]);
+      find(next + kWaves * kStep);
     }
     const bool whole = at + kStep <= fewest;  // every query sees every position of the step
     bf16x8 p[R][PTERMS];
@@ -354,10 +353,17 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) 
 #pragma unroll
           for (int t = PTERMS - 1; t >= 0; --t) o[r][4 * w + k] = mma(e[k], p[r][t], o[r][4 * w + k]);
     }
-    if (next < end) {
-      vt.load(u, slot[0], slot[1], off);
-      if (next + kWaves * kStep < end) find(next + kWaves * kStep);
-    }
+    if constexpr (MORE) vt.load(u, slot[0], slot[1], off);
+  };
+  if (at < end) {
+    find(at);
+    settle(at);
+    kt[0].load(u, slot[0], off.k[0]);
+    kt[1].load(u, slot[1], off.k[1]);
+    vt.load(u, slot[0], slot[1], off);
+    find(at + kWaves * kStep);
+    for (; at + kWaves * kStep < end; at += kWaves * kStep) step(std::true_type{});
+    step(std::false_type{});
   }
   // the four waves together: 16 queries at a time, thread (query, stretch of HD / 16 channels)
   const bool last = a.n_splits == 1;
@@ -547,7 +553,7 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a) 
 #pragma unroll
   for (int j = 0; j < BLOCKS; ++j) {
     const int blk = min(first / kBlockRows + j, (T - 1) / kBlockRows);
-    k[j].load(u, u.slot(blk), (uint32_t)min(lane & 15, T - 1 - blk * kBlockRows) * u.row_stride + (lane >> 4) * 16);
+    k[j].load(u, u.slot(u.named(blk)), (uint32_t)min(lane & 15, T - 1 - blk * kBlockRows) * u.row_stride + (lane >> 4) * 16);
   }
   float w[BLOCKS][4];
 #pragma unroll

@@ -204,7 +204,7 @@ int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens
   const int64_t keep = p->budget < p->t_max ? p->budget : p->t_max;
   if ((rc = check_cache(p, src, p->t_max))) return rc;
   if ((rc = check_cache(p, dst, keep))) return rc;
-  if (!seq_lens || !weights || !weights_out || !idx || !n_kept || !ws || weights == weights_out || lens_out == seq_lens || same_slab(src, dst))
+  if (!seq_lens || !weights || !weights_out || !idx || !n_kept || !ws || !aligned(ws) || weights == weights_out || lens_out == seq_lens || same_slab(src, dst))
     return AMS_ERR_INVALID_ARG;
   if (ws_bytes < evict_ws_bytes(p)) return AMS_ERR_WORKSPACE_TOO_SMALL;
   const Dims d = dims(p);

@@ -1,13 +1,25 @@
 // Which positions stay by accumulated attention weight (ams_evict): the first and last ones of the rules, and of the others
-// the `need` of largest weight, equal ones by lower position.  One workgroup per unit finds the need-th largest weight by its
-// digits (8 bits at a time from the top, counts in LDS; three of the four passes over the row come out of L2), then every wave
-// walks a stretch of the row and writes its kept positions behind those of the stretches before it.
+// the `need` of largest weight, equal ones by lower position.  One workgroup per unit.
+//
+// 1. The need-th largest weight, by its digits from the top, 11, 11 and 10 bits of an order-preserving integer image of the floats:
+//    counts per digit in LDS, one wave finds the digit.  Rows of up to 16 positions a thread stay in registers, so that the
+//    weights are read once.
+// 2. Two bits a position, above that weight and equal to it, in LDS; sums of their counts say where each group of 64 writes, and which of
+//    the equal ones stay.
+// Longer rows have two launches before that, since one compute unit reads its row at no more than 15 to 25 GB/s (96 rows of 40000 to
+// 131072 positions of which 4096 stay: 316 us with digits of the whole row from one workgroup, 112 with a sample and one
+// walk, 56 now): a sample of the row says between which two values the wanted one lies, then many workgroups mark what is above
+// and what is between.  The digits are those of what is between.  The sample is wrong once in some thousand rows; the counts
+// show it, and the digits of the whole row decide.
 #include "cache.h"
 
 namespace ams {
 namespace {
 
 constexpr int kWaves = 16, kThreads = 64 * kWaves;
+constexpr int kBins = 2048;
+constexpr int kSample = 4 * kThreads;
+constexpr int kMarked = 4096 * 64;  // longest row with marks
 
 // Larger weight, larger key; no number: 0, below every number (-inf: 0x007FFFFF); -0 as 0.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -16,88 +28,417 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kThreads) void evict_pick_kernel(EvictArgs a) {
-  __shared__ int bins[256];
-  __shared__ int sums[kWaves], ties[kWaves];
-  __shared__ uint32_t found[2];  // digit, keys above it
+// The value of a key, for comparisons with weights (x > value, x >= value); keys beside the numbers: the nearest number's.
+__device__ __forceinline__ float key_weight(uint32_t k) {
+  k = min(max(k, 0x007FFFFFu), 0xFF800000u);
+  if (k == 0x7FFFFFFFu) k = 0x7FFFFFFEu;  // -0 has the key of 0: the number below
+  return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+
+// Sum over the lanes above this one.
+__device__ __forceinline__ int wave_sum_above(int v, int lane) {
+  int s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_down(s, o);
+    if (lane + o < 64) s += up;
+  }
+  return s - v;
+}
+
+struct Found {
+  int digit, above, equal;  // the bin that holds the need-th largest; keys in higher bins; keys in it
+};
+
+// One wave: the bin of the need-th largest key (1 <= need <= all of them).
+__device__ __forceinline__ Found find_bin(const int* bins, int need, int lane) {
+  constexpr int PER = kBins / 64;
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; i += 4) {
+    const int4 v = *(const int4*)&bins[lane * PER + i];
+    sum += v.x + v.y + v.z + v.w;
+  }
+  int above = wave_sum_above(sum, lane);
+  const uint64_t holds = __ballot(above < need && above + sum >= need);
+  const int owner = __ffsll((unsigned long long)holds) - 1;
+  above = __shfl(above, owner);
+  const int mine = lane < PER ? bins[owner * PER + lane] : 0;
+  const int over = above + wave_sum_above(mine, lane);
+  const uint64_t here = __ballot(over < need && over + mine >= need);
+  const int at = __ffsll((unsigned long long)here) - 1;
+  return Found{owner * PER + at, __shfl(over, at), __shfl(mine, at)};
+}
+
+template <int PER>
+struct PickLds {
+  static constexpr int kWords = PER ? 16 * PER : kMarked / 64;  // groups of 64 positions whose bits are here at a time
+  static constexpr int kList = PER ? 1 : 16384;                 // kept positions that are written at a time, from a list
+  static constexpr int kBetween = PER ? 4 : 8192;               // positions between the sample's bounds
+  uint64_t over[kWords], tie[kWords];
+  union {
+    struct {
+      __align__(16) int bins[2][kBins];
+      uint32_t key[kBetween];
+      int32_t where[kBetween];
+    };
+    int32_t list[kList];
+    int32_t slot[PER ? kWords : 1];  // kept positions before the group
+  };
+  int sums[kWaves], tie_sums[kWaves];
+  Found found;
+};
+
+// What precedes evict_pick_kernel for long rows, in the workspace: per unit the sample's bounds, and two bits a position.
+struct Marks {
+  float2* bounds;          // null: no marks
+  uint64_t *over, *between;  // [units, words]
+  int words;
+};
+
+// How many of the row's candidates [from, to) are wanted.
+struct Rule {
+  int T, kept, from, to, wanted;
+  __device__ __forceinline__ Rule(const EvictArgs& a, int b) {
+    T = seq_len(a.d, a.seq_lens, b);
+    kept = min(a.budget, T);
+    const int sinks = min(a.n_sink, kept), last = min(a.n_last, kept - sinks);
+    from = sinks, to = T - last;
+    wanted = kept - sinks - last;  // 0 .. to - from
+  }
+  __device__ __forceinline__ bool marked() const { return wanted > 0 && wanted < to - from && to - from > 4 * kSample; }
+};
+
+// Values between which the wanted one lies, from runs of four weights: exact ones of the sample, seven deviations of independent draws
+// each way (neighbours resemble each other), fewer where that would leave more than four fifths of what can be kept between.
+__global__ __launch_bounds__(kThreads) void evict_bounds_kernel(EvictArgs a, Marks m) {
+  __shared__ __align__(16) int bins[2][kBins];
+  __shared__ Found found[2];
   const int unit = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
-  const int T = seq_len(a.d, a.seq_lens, b);
-  const int kept = min(a.budget, T), sinks = min(a.n_sink, kept), last = min(a.n_last, kept - sinks);
-  const int from = sinks, to = T - last;  // candidates
+  const Rule r(a, b);
+  if (!r.marked()) return;
+  const float* w = a.weights + (int64_t)unit * a.d.t_stride;
+  const int n = r.to - r.from;
+  const double share = (double)r.wanted / n, mean = share * kSample;
+  const int margin = (int)fmin(7.0 * sqrt(mean * (1 - share)), 0.4 * PickLds<0>::kBetween * kSample / n) + 4;
+  const int rank[2] = {(int)mean - margin, (int)mean + margin};
+  uint32_t key[4], bound[2] = {0, 0};
+  int left[2] = {min(max(rank[0], 1), kSample), min(max(rank[1], 1), kSample)};
+  const int run = r.from + (int)((int64_t)threadIdx.x * (n - 4) / kThreads);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) key[i] = weight_key(w[run + i]);
+#pragma unroll
+  for (int shift = 21; shift >= 0; shift -= shift == 21 ? 11 : 10) {
+    const uint32_t mask = shift == 21 ? 0u : ~0u << (shift == 10 ? 21 : 10);
+    for (int i = threadIdx.x; i < 2 * kBins; i += kThreads) bins[0][i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if ((key[i] & mask) == bound[k]) atomicAdd(&bins[k][key[i] >> shift & (shift == 0 ? 1023 : 2047)], 1);
+    __syncthreads();
+    if (wave < 2) {
+      const Found f = find_bin(bins[wave], wave ? left[1] : left[0], lane);
+      if (lane == 0) found[wave] = f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      bound[k] |= (uint32_t)found[k].digit << shift;
+      left[k] -= found[k].above;
+    }
+  }
+  if (threadIdx.x == 0)
+    m.bounds[unit] = make_float2(rank[1] > kSample ? -INFINITY : key_weight(bound[1]), rank[0] < 1 ? INFINITY : key_weight(bound[0]));
+}
+
+constexpr int kMarkThreads = 256, kMarkGroups = 16;                   // groups of 64 positions per wave
+constexpr int kMarkPositions = kMarkThreads / 64 * kMarkGroups * 64;  // per workgroup
+
+// The bits of the row, and the zeros behind the kept weights.
+__global__ __launch_bounds__(kMarkThreads) void evict_mark_kernel(EvictArgs a, Marks m) {
+  const int unit = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  int l, b, h;
+  unit_coords(a.d, unit, l, b, h);
+  const Rule r(a, b);
+  const int t0 = blockIdx.x * kMarkPositions + wave * kMarkGroups * 64;
+  float* out = a.weights_out + (int64_t)unit * a.d.t_stride;
+#pragma unroll
+  for (int g = 0; g < kMarkGroups; ++g) {
+    const int t = t0 + g * 64 + lane;
+    if (t >= r.kept && t < a.d.t_max) out[t] = 0.f;
+  }
+  if (!r.marked() || t0 >= r.T) return;
+  const float* w = a.weights + (int64_t)unit * a.d.t_stride;
+  const float2 bound = m.bounds[unit];
+  float x[kMarkGroups];
+#pragma unroll
+  for (int g = 0; g < kMarkGroups; ++g) x[g] = w[min(t0 + g * 64 + lane, r.T - 1)];
+  uint64_t my_over = 0, my_between = 0;
+#pragma unroll
+  for (int g = 0; g < kMarkGroups; ++g) {
+    const int t = t0 + g * 64 + lane;
+    const bool in = t >= r.from && t < r.to;
+    const uint64_t over = __ballot(in ? x[g] > bound.y : t < r.T), between = __ballot(in && x[g] >= bound.x && !(x[g] > bound.y));
+    if (lane == g) my_over = over, my_between = between;
+  }
+  const int word = t0 / 64 + lane;
+  if (lane < kMarkGroups && word < m.words) {
+    m.over[(int64_t)unit * m.words + word] = my_over;
+    m.between[(int64_t)unit * m.words + word] = my_between;
+  }
+}
+
+// PER: positions per thread whose weights stay in registers; 0: any length, from memory.
+template <int PER>
+__global__ __launch_bounds__(kThreads) void evict_pick_kernel(EvictArgs a, Marks m) {
+  __shared__ PickLds<PER> s;
+  const int unit = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  int l, b, h;
+  unit_coords(a.d, unit, l, b, h);
+  const Rule rule(a, b);
+  const int T = rule.T, kept = rule.kept, from = rule.from, to = rule.to, wanted = rule.wanted;
   const float* w = a.weights + (int64_t)unit * a.d.t_stride;
   float* out = a.weights_out + (int64_t)unit * a.d.t_stride;
   int32_t* idx = a.idx + (int64_t)unit * a.budget;
-  // the need-th largest key: its digits, and how many of the keys equal to it stay
-  int need = kept - sinks - last;
-  uint32_t key = 0u, mask = 0u;
-  if (need < to - from && need > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = threadIdx.x; i < 256; i += kThreads) bins[i] = 0;
-      __syncthreads();
-      for (int t = from + (int)threadIdx.x; t < to; t += kThreads) {
-        const uint32_t k = weight_key(w[t]);
-        if ((k & mask) == key) atomicAdd(&bins[k >> shift & 255], 1);
-      }
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        int above = 0, digit = 255;
-        while (above + bins[digit] < need) above += bins[digit--];
-        found[0] = digit, found[1] = above;
-      }
-      __syncthreads();
-      key |= found[0] << shift;
-      mask |= 255u << shift;
-      need -= (int)found[1];
-      __syncthreads();
-    }
-  } else if (need > 0) {
-    need = 0, key = 0u, mask = 0u;  // all of them stay (below)
-  } else {
-    mask = 1u;  // none of them
-  }
-  const bool all = mask == 0u, none = mask == 1u;
-  // where each wave's stretch writes
-  const int per = ((T + kWaves - 1) / kWaves + 63) & ~63, lo = min(T, wave * per), hi = min(T, lo + per);
-  int above = 0, equal = 0;
-  for (int t = lo + lane; t < hi; t += 64) {
-    const bool always = t < from || t >= to;
-    const uint32_t k = always || all || none ? 0u : weight_key(w[t]);
-    above += always || all || (!none && k > key);
-    equal += !always && !all && !none && k == key;
-  }
+  constexpr int kWords = PickLds<PER>::kWords, kPerThread = (kWords + kThreads - 1) / kThreads;
+
+  // f(first position, the lane's weight) for the groups of 64 positions of [begin, end) that are the wave's, whose lengths end at T
+  float held[PER ? PER : 1];
+  if constexpr (PER > 0) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) above += __shfl_xor(above, o), equal += __shfl_xor(equal, o);
-  if (lane == 0) sums[wave] = above, ties[wave] = equal;
-  __syncthreads();
-  int slot = 0, tied = 0;  // kept positions, equal keys before this stretch
-  for (int v = 0; v < wave; ++v) slot += sums[v], tied += ties[v];
-  slot += min(tied, need);
-  for (int t0 = lo; t0 < hi; t0 += 64) {
-    const int t = t0 + lane;
-    bool stays = false, tie = false;
-    float x = 0.f;
-    if (t < hi) {
-      const bool always = t < from || t >= to;
-      x = w[t];
-      const uint32_t k = weight_key(x);
-      stays = always || all || (!none && k > key);
-      tie = !always && !all && !none && k == key;
+    for (int g = 0; g < PER; ++g) {
+      const int t = (wave * PER + g) * 64 + lane;
+      held[g] = t < T ? w[t] : 0.f;
     }
-    const uint64_t before = (1ull << lane) - 1, tie_set = __ballot(tie);
-    stays = stays || (tie && tied + __popcll(tie_set & before) < need);
-    const uint64_t set = __ballot(stays);
-    if (stays) {
-      const int j = slot + __popcll(set & before);
-      idx[j] = t;
-      out[j] = x;
+  }
+  auto walk = [&](int begin, int end, auto f) __attribute__((always_inline)) {
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int g = 0; g < PER; ++g)
+        if ((wave * PER + g) * 64 < T) f((wave * PER + g) * 64, held[g]);
+    } else {
+      constexpr int AHEAD = 8;  // groups in flight: one workgroup has the latency of its row to itself
+      float next[AHEAD];
+      auto fetch = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < AHEAD; ++g) next[g] = w[min(t0 + g * 64 + lane, T - 1)];
+      };
+      int t0 = begin + wave * AHEAD * 64;
+      if (t0 < end) fetch(t0);
+      for (; t0 < end; t0 += kWaves * AHEAD * 64) {
+        float x[AHEAD];
+#pragma unroll
+        for (int g = 0; g < AHEAD; ++g) x[g] = next[g];
+        fetch(t0 + kWaves * AHEAD * 64);  // (whatever comes: a load under a condition makes every wait one for all loads)
+#pragma unroll
+        for (int g = 0; g < AHEAD; ++g)
+          if (t0 + g * 64 < end) f(t0 + g * 64, x[g]);
+      }
     }
-    slot += __popcll(set);
-    tied += __popcll(tie_set);
+  };
+  // Counts of one digit are in bins[turn] (the first ones cleared by clear_bins, the others by find, whose other waves have time).
+  int turn = 0;
+  auto clear_bins = [&]() __attribute__((always_inline)) {
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[0][i] = 0;
+    turn = 0;
+    __syncthreads();
+  };
+  auto find = [&](int need) __attribute__((always_inline)) {
+    __syncthreads();
+    if (wave == 0) {
+      const Found f = find_bin(s.bins[turn], need, lane);
+      if (lane == 0) s.found = f;
+    } else {
+      for (int i = threadIdx.x - 64; i < kBins; i += kThreads - 64) s.bins[turn ^ 1][i] = 0;
+    }
+    turn ^= 1;
+    __syncthreads();
+    return s.found;
+  };
+  auto before = [&](int v, int* sums, int& sum) __attribute__((always_inline)) {  // sum over lower threads; over all
+    int run = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int down = __shfl_up(run, o);
+      if (lane >= o) run += down;
+    }
+    if (lane == 63) sums[wave] = run;
+    __syncthreads();
+    int under = 0;
+    sum = 0;
+    for (int v2 = 0; v2 < kWaves; ++v2) {
+      const int x = sums[v2];
+      under += v2 < wave ? x : 0;
+      sum += x;
+    }
+    return under + run - v;
+  };
+
+  const bool all = wanted == to - from;
+  // keys above top stay, and of low .. top the first `ties`
+  uint32_t low = 0, top = 0;
+  int ties = 0;
+  bool done = all || wanted == 0, marked = false;
+  if constexpr (PER == 0) {
+    if (m.bounds && rule.marked()) {
+      const int words = (T + 63) / 64;
+      uint64_t between[kPerThread];
+      int n_over = 0, n_between = 0, total, n;
+#pragma unroll
+      for (int i = 0; i < kPerThread; ++i) {
+        const int g = threadIdx.x * kPerThread + i;
+        between[i] = g < words ? m.between[(int64_t)unit * m.words + g] : 0ull;
+        const uint64_t over = g < words ? m.over[(int64_t)unit * m.words + g] : 0ull;
+        s.over[g] = over, s.tie[g] = 0ull;
+        n_over += __popcll(over), n_between += __popcll(between[i]);
+      }
+      int at = before(n_between, s.tie_sums, n);
+      before(n_over, s.sums, total);
+      const int need = kept - total;  // (the bits above hold those that stay whatever their weight)
+      const float2 bound = m.bounds[unit];
+      if (need >= 1 && need <= n && (n <= PickLds<0>::kBetween || bound.x == bound.y)) {
+        marked = done = true;
+        ties = need;
+        if (bound.x == bound.y) {  // equal ones, all of them
+#pragma unroll
+          for (int i = 0; i < kPerThread; ++i) s.tie[threadIdx.x * kPerThread + i] = between[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPerThread; ++i)
+            for (uint64_t set = between[i]; set; set &= set - 1)
+              s.where[at++] = (threadIdx.x * kPerThread + i) * 64 + __ffsll((unsigned long long)set) - 1;
+          __syncthreads();
+          for (int i = threadIdx.x; i < n; i += kThreads) s.key[i] = weight_key(w[s.where[i]]);
+          clear_bins();
+#pragma unroll
+          for (int shift = 21; shift >= 0; shift -= shift == 21 ? 11 : 10) {
+            const uint32_t mask = shift == 21 ? 0u : ~0u << (shift == 10 ? 21 : 10);
+            for (int i = threadIdx.x; i < n; i += kThreads)
+              if ((s.key[i] & mask) == low) atomicAdd(&s.bins[turn][s.key[i] >> shift & (shift == 0 ? 1023 : 2047)], 1);
+            const Found f = find(ties);
+            low |= (uint32_t)f.digit << shift;
+            ties -= f.above;
+          }
+          for (int i = threadIdx.x; i < n; i += kThreads) {
+            const int t = s.where[i];
+            if (s.key[i] >= low)
+              atomicOr((unsigned long long*)(s.key[i] > low ? &s.over[t >> 6] : &s.tie[t >> 6]), 1ull << (t & 63));
+          }
+        }
+      }
+      __syncthreads();
+    }
+  }
+  if (!done) {
+    int need = wanted;
+    clear_bins();
+    for (int shift = 21;; shift -= shift == 21 ? 11 : 10) {
+      const uint32_t mask = shift == 21 ? 0u : ~0u << (shift == 10 ? 21 : 10);
+      walk(0, T, [&](int t0, float x) __attribute__((always_inline)) {
+        const uint32_t k = weight_key(x);
+        if (t0 + lane >= from && t0 + lane < to && (k & mask) == low) atomicAdd(&s.bins[turn][k >> shift & (shift == 0 ? 1023 : 2047)], 1);
+      });
+      const Found f = find(need);
+      low |= (uint32_t)f.digit << shift;
+      need -= f.above;
+      top = low | (shift == 0 ? 0u : (1u << shift) - 1u);
+      ties = need;
+      if (f.equal == need || shift == 0) break;  // all that share the digits stay; or there are no more digits
+    }
+    __syncthreads();  // the bins have been read
+  }
+
+  // By value where low and top are numbers' keys; no numbers among the ties: by key.
+  const bool some = !all && wanted > 0, odd = some && low < 0x007FFFFFu;
+  const float f_low = key_weight(low), f_top = key_weight(top);
+  int slot0 = 0, rank0 = 0;  // kept positions, ties before the round
+  for (int begin = 0; begin < T; begin += kWords * 64) {
+    const int end = min(T, begin + kWords * 64), words = (end - begin + 63) / 64;
+    if (!marked) walk(begin, end, [&](int t0, float x) __attribute__((always_inline)) {
+      uint64_t over = 0, tie = 0;
+      if (some) {
+        if (!odd) {
+          over = __ballot(x > f_top), tie = __ballot(x >= f_low) & ~over;
+        } else {
+          const uint32_t k = weight_key(x);
+          over = __ballot(k > top), tie = __ballot(k >= low) & ~over;
+        }
+      }
+      if (t0 < from || t0 + 64 > to) {
+        const uint64_t always = __ballot(t0 + lane < T && (all || t0 + lane < from || t0 + lane >= to)), in = __ballot(t0 + lane < T);
+        over = (over & in) | always, tie = tie & in & ~always;
+      } else if (all) {
+        over = ~0ull;
+      }
+      if (lane == 0) s.over[(t0 - begin) >> 6] = over, s.tie[(t0 - begin) >> 6] = tie;
+    });
+    __syncthreads();
+    // ties before every group, then what stays of them, then the kept positions before it
+    uint64_t over[kPerThread], tie[kPerThread];
+    int n_tie = 0;
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const int g = threadIdx.x * kPerThread + i;
+      over[i] = g < words ? s.over[g] : 0ull, tie[i] = g < words ? s.tie[g] : 0ull;
+      n_tie += __popcll(tie[i]);
+    }
+    int round_ties, round_kept;
+    int rank = rank0 + before(n_tie, s.tie_sums, round_ties), n_kept = 0;
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const int n = __popcll(tie[i]);
+      if (rank + n > ties) {  // the first ties - rank of them
+        const int stay = max(0, ties - rank);
+        uint64_t rest = tie[i];
+        for (int k = 0; k < stay; ++k) rest &= rest - 1;
+        tie[i] &= ~rest;
+      }
+      rank += n;
+      over[i] |= tie[i];
+      n_kept += __popcll(over[i]);
+    }
+    int slot = slot0 + before(n_kept, s.sums, round_kept);
+    if constexpr (PER > 0) {  // the weights are in the registers of the waves that walk the row
+      if (threadIdx.x < kWords) s.over[threadIdx.x] = over[0], s.slot[threadIdx.x] = slot;
+      __syncthreads();
+      walk(begin, end, [&](int t0, float x) __attribute__((always_inline)) {
+        const uint64_t set = s.over[t0 >> 6];
+        if (set >> lane & 1) {
+          const int j = s.slot[t0 >> 6] + __popcll(set & ((1ull << lane) - 1));
+          idx[j] = t0 + lane, out[j] = x;
+        }
+      });
+    } else {
+      for (int base = 0; base < round_kept; base += PickLds<PER>::kList) {  // through a list of positions, so that loads and stores are dense
+        int at = slot - slot0 - base;
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+          const int n = __popcll(over[i]);
+          if (at + n > 0 && at < PickLds<PER>::kList) {
+            int k = at;
+            for (uint64_t set = over[i]; set; set &= set - 1, ++k)
+              if (k >= 0 && k < PickLds<PER>::kList) s.list[k] = begin + (threadIdx.x * kPerThread + i) * 64 + __ffsll((unsigned long long)set) - 1;
+          }
+          at += n;
+        }
+        __syncthreads();
+        for (int j = threadIdx.x; j < min(round_kept - base, PickLds<PER>::kList); j += kThreads) {
+          const int t = s.list[j];
+          idx[slot0 + base + j] = t, out[slot0 + base + j] = w[t];
+        }
+        __syncthreads();
+      }
+    }
+    slot0 += round_kept, rank0 += round_ties;
+    __syncthreads();  // before the next round's bits
   }
   for (int j = kept + (int)threadIdx.x; j < a.budget; j += kThreads) idx[j] = -1;
-  for (int j = kept + (int)threadIdx.x; j < a.d.t_max; j += kThreads) out[j] = 0.f;
+  if (!m.bounds)  // else they are there
+    for (int j = kept + (int)threadIdx.x; j < a.d.t_max; j += kThreads) out[j] = 0.f;
   if (threadIdx.x == 0) {
     a.n_kept[unit] = kept;
     if (a.lens_out && l == 0 && h == 0) a.lens_out[b] = kept;
@@ -106,11 +447,30 @@ __global__ __launch_bounds__(kThreads) void evict_pick_kernel(EvictArgs a) {
 
 }  // namespace
 
-size_t evict_ws_bytes(const ams_params*) { return 256; }
+static size_t mark_words(int t_max) { return t_max > 16 * kThreads && t_max <= kMarked ? (size_t)div_up(t_max, 64) : 0; }
 
-hipError_t launch_evict_pick(const EvictArgs& a, char*, hipStream_t s) {
+size_t evict_ws_bytes(const ams_params* p) {
+  const size_t units = (size_t)p->n_layers * p->batch * p->n_kv_heads;
+  return 256 + units * (2 * mark_words(p->t_max) * sizeof(uint64_t) + sizeof(float2));
+}
+
+hipError_t launch_evict_pick(const EvictArgs& a, char* ws, hipStream_t s) {
+  Marks m{};
+  if (const size_t words = mark_words(a.d.t_max)) {
+    m.over = (uint64_t*)ws, m.between = m.over + a.d.units * words, m.bounds = (float2*)(m.between + a.d.units * words);
+    m.words = (int)words;
+    prof_mark("evict_bounds", s);
+    hipLaunchKernelGGL(evict_bounds_kernel, dim3(a.d.units), dim3(kThreads), 0, s, a, m);
+    prof_mark("evict_mark", s);
+    hipLaunchKernelGGL(evict_mark_kernel, dim3(div_up(a.d.t_max, kMarkPositions), a.d.units), dim3(kMarkThreads), 0, s, a, m);
+  }
   prof_mark("evict_pick", s);
-  hipLaunchKernelGGL(evict_pick_kernel, dim3(a.d.units), dim3(kThreads), 0, s, a);
+  if (a.d.t_max <= 4 * kThreads)
+    hipLaunchKernelGGL((evict_pick_kernel<4>), dim3(a.d.units), dim3(kThreads), 0, s, a, m);
+  else if (a.d.t_max <= 16 * kThreads)
+    hipLaunchKernelGGL((evict_pick_kernel<16>), dim3(a.d.units), dim3(kThreads), 0, s, a, m);
+  else
+    hipLaunchKernelGGL((evict_pick_kernel<0>), dim3(a.d.units), dim3(kThreads), 0, s, a, m);
   return hipGetLastError();
 }
 

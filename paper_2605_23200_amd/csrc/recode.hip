@@ -2,13 +2,48 @@
 // value = code * scale of its block of 16 positions; a destination block takes the scale of the largest magnitude of ITS 16
 // rows, so a block is the unit of work: one wave holds all of it in registers (eight elements per lane and row: 16 lanes a
 // row of 128 channels, four rows a load), reduces the largest magnitude over its lanes and writes codes and scale.  Every byte
-// moves once; no LDS, no barrier.  Memory is the bound.
+// moves once; no LDS, no barrier.  Memory is the bound: what a gathered row waits for (index, page, then scale and row) is a
+// chain of latencies, so a wave starts all rows of K and V of its block before it looks at the first.
 #include "cache.h"
 
 namespace ams {
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+// Eight elements as they lie in memory.
+template <int EL>
+struct Raw {
+  uint32_t w[EL == EL_F32 ? 8 : EL == EL_BF16 ? 4 : 2];
+  __device__ __forceinline__ void load(const char* at) {
+    if constexpr (kPacked<EL>) {
+      const uint2 a = *(const uint2*)at;
+      w[0] = a.x, w[1] = a.y;
+    } else {
+      const uint4 a = *(const uint4*)at;
+      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+      if constexpr (EL == EL_F32) {
+        const uint4 b = *(const uint4*)(at + 16);
+        w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+      }
+    }
+  }
+  __device__ __forceinline__ void values(float (&x)[8]) const {
+    if constexpr (EL == EL_F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    } else if constexpr (EL == EL_BF16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    } else {
+      float lo[4], hi[4];
+      unpack_codes<EL>(w[0], lo);
+      unpack_codes<EL>(w[1], hi);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = lo[i], x[4 + i] = hi[i];
+    }
+  }
+};
 
 template <int SRC, int DST, int HD>
 __global__ __launch_bounds__(kThreads) void recode_kernel(RecodeArgs a) {
@@ -17,66 +52,76 @@ __global__ __launch_bounds__(kThreads) void recode_kernel(RecodeArgs a) {
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const bool values = wave & 1;
-  const int blk = blockIdx.x * (kWaves / 2) + (wave >> 1);
-  const int most = min(a.budget, a.d.t_max);
-  const int n = a.idx ? min(a.n_kept[unit], most) : seq_len(a.d, a.seq_lens, b);
+  const int blk = blockIdx.x * kWaves + wave;
+  const int n = a.idx ? min(a.n_kept[unit], min(a.budget, a.d.t_max)) : seq_len(a.d, a.seq_lens, b);
   if (blk * kBlockRows >= n) return;
-  const CacheDev src = values ? a.vs : a.ks, dst = values ? a.vd : a.kd;
   const int32_t* idx = a.idx ? a.idx + (int64_t)unit * a.budget : nullptr;
   const int i = lane % LANES, r0 = lane / LANES;
-  float x[PASSES][8];
-  uint32_t top = 0;
+  int t[PASSES];
+  bool real[PASSES];  // false: a row of zeros (an index outside the cache), or none
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
-    const int j = blk * kBlockRows + p * ROWS + r0;
-    int t = -1;
-    if (j < n) t = idx ? idx[j] : j;
-    if (t < 0 || t >= a.d.t_max) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[p][e] = 0.f;
-      continue;
-    }
-    const Block s = block_at(src, l, b, h, t / kBlockRows);
-    load_eight<SRC>(s.row0 + (t % kBlockRows) * s.stride + i * 8 * kElBytes<SRC>, x[p]);
-    if constexpr (kPacked<SRC>) {
-      const float scale = src.scale[s.scale];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[p][e] *= scale;
-    }
+    const int j = min(blk * kBlockRows + p * ROWS + r0, n - 1);
+    t[p] = idx ? idx[j] : j;
   }
-  const Block to = block_at(dst, l, b, h, blk);
-  if (to.there) {
+  if (idx && a.credit_src && a.credit_dst && lane < kBlockRows) {
+    const int j = blk * kBlockRows + lane, from = j < n ? idx[j] : -1;
+    if (from >= 0 && from < a.d.t_max)
+      a.credit_dst[(int64_t)unit * a.credit_dst_stride + j] = a.credit_src[(int64_t)unit * a.d.t_stride + from];
+  }
+  Raw<SRC> raw[2][PASSES];
+  float scale[2][PASSES];
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    real[p] = t[p] >= 0 && t[p] < a.d.t_max;
+    const int from = real[p] ? t[p] : 0;
+    const Block s = block_at(a.ks, l, b, h, from / kBlockRows);  // V lies in the same places
+    const int64_t at = (s.row0 - a.ks.base) + (from % kBlockRows) * s.stride + i * 8 * kElBytes<SRC>;
+    raw[0][p].load(a.ks.base + at);
+    raw[1][p].load(a.vs.base + at);
+    scale[0][p] = kPacked<SRC> ? a.ks.scale[s.scale] : 1.f;
+    scale[1][p] = kPacked<SRC> ? a.vs.scale[s.scale] : 1.f;
+  }
+  const Block to = block_at(a.kd, l, b, h, blk);
+  if (!to.there) return;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    const CacheDev& dst = kv ? a.vd : a.kd;
+    float x[PASSES][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      raw[kv][p].values(x[p]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (kPacked<SRC>) x[p][e] *= scale[kv][p];
+        if (!real[p]) x[p][e] = 0.f;
+      }
+      if constexpr (kPacked<DST>) top = top_bits(x[p], top);
+    }
     float inverse = 1.f;
     if constexpr (kPacked<DST>) {
-#pragma unroll
-      for (int p = 0; p < PASSES; ++p) top = top_bits(x[p], top);
-      const float scale = block_scale<DST>(wave_max(top));
-      inverse = scale_inverse(scale);
-      if (lane == 0) dst.scale[to.scale] = scale;
+      const float s = block_scale<DST>(wave_max(top));  // (the last row stands in for those behind it)
+      inverse = scale_inverse(s);
+      if (lane == 0) dst.scale[to.scale] = s;
     }
+    char* rows = dst.base + (to.row0 - a.kd.base) + i * 8 * kElBytes<DST>;
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       const int r = p * ROWS + r0;
       if (blk * kBlockRows + r >= n) continue;
-      char* row = to.row0 + r * to.stride + i * 8 * kElBytes<DST>;
       if constexpr (kPacked<DST>)
-        *(uint2*)row = pack_eight<DST>(x[p], inverse);
+        *(uint2*)(rows + r * to.stride) = pack_eight<DST>(x[p], inverse);
       else
-        store_eight<DST>(row, x[p]);
+        store_eight<DST>(rows + r * to.stride, x[p]);
     }
-  }
-  if (!values && idx && a.credit_src && a.credit_dst && lane < kBlockRows) {
-    const int j = blk * kBlockRows + lane;
-    if (j < n && idx[j] >= 0 && idx[j] < a.d.t_max)
-      a.credit_dst[(int64_t)unit * a.credit_dst_stride + j] = a.credit_src[(int64_t)unit * a.d.t_stride + idx[j]];
   }
 }
 
 template <int SRC, int DST>
 hipError_t launch(const RecodeArgs& a, hipStream_t s) {
   const int rows = a.idx ? min(a.budget, a.d.t_max) : a.d.t_max;
-  const dim3 grid(div_up(rows, kBlockRows * (kWaves / 2)), a.d.units);
+  const dim3 grid(div_up(rows, kBlockRows * kWaves), a.d.units);
   prof_mark("recode", s);
   if (a.d.D == 128)
     hipLaunchKernelGGL((recode_kernel<SRC, DST, 128>), grid, dim3(kThreads), 0, s, a);

@@ -653,6 +653,70 @@ def test_evict_long_rows(T):
     _evict_case(src, HostCache("e4m3", shape, T // 8, False, 20), w, lens, T // 8, 4, 32)
 
 
+def test_evict_rows_that_mislead_a_sample():
+    """Rows longer than a sample of them: weights that a regular stride sees wrongly (so that its bounds miss), one outlier, few distinct
+    values, almost everything kept or nothing, no numbers and infinities everywhere."""
+    T, D = 50000, 64
+    rng = np.random.default_rng(8)
+    w = rng.random((10, T + 4)).astype(np.float32)
+    w[0, ::3] += 5                                      # periods
+    w[1, (np.arange(16384, dtype=np.int64) * T) // 16384] = 0          # what a sample of 16384 sees
+    w[2, (np.arange(16384, dtype=np.int64) * (T - 36)) // 16384 + 4] = 2   # the same past 4 + 32 kept ones
+    w[3] = 1.0
+    w[4] = rng.integers(0, 2, T + 4)
+    w[5] = 0
+    w[5, 777] = 1
+    w[6] = np.nan
+    w[6, 5:9000] = -1
+    w[7] = np.where(rng.random(T + 4) < 0.3, np.nan, rng.choice(np.array([np.inf, -np.inf, -0.0, 0.0], np.float32), T + 4))
+    w[8] = -np.exp(rng.standard_normal(T + 4))
+    w[9] = np.float32(1) + rng.integers(0, 3000, T + 4).astype(np.float32) * np.float32(2.0 ** -23)
+    _evict_lists(w, [T] * 9 + [T - 1], D, ((40, 4, 32), (3000, 0, 0), (25000, 4, 32), (49990, 1, 1)))
+
+
+@pytest.mark.parametrize("T", [16384, 16385, 262144, 262145, 600001])
+def test_evict_rows_of_every_kind_of_length(T):
+    """The longest rows in registers, the shortest and longest with marks, rows whose bits take several rounds; short rows among them."""
+    rng = np.random.default_rng(T)
+    w = np.exp(2 * rng.standard_normal((4, T + 3))).astype(np.float32)
+    w[2, : T // 2] = 0.25
+    _evict_lists(w, [T, 9000, T - 63, 17000 if T > 17000 else 100], 64, ((3000, 4, 32), (T // 3 * 2, 0, 5)))
+
+
+def _evict_lists(w, lens, D, rules):
+    """Kept positions and their weights alone (the rows are not what is looked at)."""
+    T, n_rows = max(lens), len(lens)
+    shape = (1, n_rows, 1, D)
+    src = HostCache("int8", shape, T)
+    for name in ("k", "v"):
+        src.t[name].fill_(1)
+    src = src.upload()
+    for budget, n_sink, n_last in rules:
+        for stride in (T, T + 3):                       # rows that are and are not 16-byte aligned
+            p = params(shape, T, budget=budget, n_sink=n_sink, n_last=n_last, t_stride=stride)
+            ww = np.ascontiguousarray(w[:, :stride])
+            dst = HostCache("int8", shape, budget).upload()
+            out, idx = torch.full((n_rows, stride), -5.0, device=DEV), torch.full((n_rows, budget), -9, dtype=torch.int32, device=DEV)
+            n_kept = torch.zeros(n_rows, dtype=torch.int32, device=DEV)
+            B.ams_evict(p, src, lens_dev(lens), torch.from_numpy(ww).to(DEV), dst, out, idx, n_kept,
+                        torch.zeros(B.ams_evict_workspace_bytes(p), dtype=torch.uint8, device=DEV))
+            idx, out = idx.cpu().numpy(), out.cpu().numpy()
+            for u in range(n_rows):
+                x, n = ww[u], lens[u]
+                kept = min(budget, n)
+                sinks = min(n_sink, kept)
+                last = min(n_last, kept - sinks)
+                nan = np.isnan(x[:n])
+                middle = np.arange(sinks, n - last)
+                order = np.lexsort((middle, -np.where(nan, 0, x[:n])[middle], nan[middle]))
+                want = np.sort(np.concatenate([np.arange(sinks), middle[order[:kept - sinks - last]], np.arange(n - last, n)]))
+                assert int(n_kept[u]) == kept
+                np.testing.assert_array_equal(idx[u, :kept], want, err_msg=f"{u} {budget}")
+                assert (idx[u, kept:] == -1).all()
+                np.testing.assert_array_equal(out[u, :kept].view(np.uint32), x[want].view(np.uint32))
+                assert (out[u, kept:T] == 0).all() and (out[u, T:] == -5).all()
+
+
 # ---- together ---------------------------------------------------------------------------------------------------
 
 def _loop_state(kind, steps, seed=0, paged=False):
