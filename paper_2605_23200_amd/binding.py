@@ -299,40 +299,41 @@ def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, device: torc
     """Pointer of a contiguous tensor of at least `numel` elements on the call's GPU; None stays None."""
     if t is None:
         return None
-    if t.device != device or t.dtype != dtype or t.numel() < numel or not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != device.index or t.numel() < numel or not t.is_contiguous():
         raise ValueError(f"{what}: contiguous {dtype} tensor of at least {numel} elements on {device} expected")
     return t.data_ptr()
 
 
 def _launch(fn, what: str, device: torch.device, stream, *args):
     """Calls fn on the cache's GPU, whichever is current, and on that GPU's current stream unless one is given."""
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, _stream(stream))
+    index = device.index
+    # (the raw handle of the current stream: making a Stream object of it costs as much as a launch)
+    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if torch._C._cuda_getDevice() == index:
+        rc = fn(*args, handle)
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, _stream(stream))
-    _check(rc, what)
+            rc = fn(*args, handle)
+    if rc != OK:
+        raise AmsError(rc, what)
+
+
+_ROWS = {F32: torch.float32, BF16: torch.bfloat16}
 
 
 def _rows_dtype(p: Params) -> torch.dtype:
-    return torch.float32 if p.kv_dtype == F32 else torch.bfloat16
+    return _ROWS[p.kv_dtype]
 
 
-def _token_rows(t: torch.Tensor, p: Params, heads: int, n_new: int, dtype, device, what: str):
+def _token_rows(t: torch.Tensor, shape, dtype, device, what: str):
     """(pointer, elements from token to token) of [L, B, n_new, heads, D]: any slice of a projection's output along the heads."""
+    L, batch, n_new, heads, D = shape
     s = t.stride()
-    if (t.device != device or t.dtype != dtype or t.shape != (p.n_layers, p.batch, n_new, heads, p.head_dim) or s[4] != 1
-            or (heads > 1 and s[3] != p.head_dim)):
-        raise ValueError(f"{what}: {dtype} [layers, batch, new, {heads}, {p.head_dim}] on {device} with contiguous heads expected")
-    for stride, n, want in ((s[1], p.batch, s[2] * n_new), (s[0], p.n_layers, s[2] * n_new * p.batch)):
-        if n > 1 and n_new > 1 and stride != want:
-            raise ValueError(f"{what}: one stride from token to token expected")
-    step = s[2]
-    if n_new == 1:                      # the tokens are those of the batch, then of the layers
-        step = s[1] if p.batch > 1 else s[0] if p.n_layers > 1 else max(s[2], heads * p.head_dim)
-        if p.batch > 1 and p.n_layers > 1 and s[0] != step * p.batch:
-            raise ValueError(f"{what}: one stride from token to token expected")
-    elif n_new > 1 and p.batch == 1 and p.n_layers > 1 and s[0] != s[2] * n_new:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device.index or s[4] != 1 or (heads > 1 and s[3] != D):
+        raise ValueError(f"{what}: {dtype} {list(shape)} (layers, batch, new, heads, channels) on {device} with contiguous heads expected")
+    # one stride from token to token, over those of a sequence, the batch and the layers (extents of one have none)
+    step = s[2] if n_new > 1 else s[1] if batch > 1 else s[0] if L > 1 else heads * D
+    if (batch > 1 and s[1] != step * n_new) or (L > 1 and s[0] != step * n_new * batch):
         raise ValueError(f"{what}: one stride from token to token expected")
     return t.data_ptr(), step
 
@@ -340,18 +341,16 @@ def _token_rows(t: torch.Tensor, p: Params, heads: int, n_new: int, dtype, devic
 def ams_append(p, q, k, v, q_weight, k_weight, norm_eps, rope, positions, seq_lens, q_out, dst, lens_out=None, stream=None):
     """q [L, B, n_new, H * G, D] (or None, q_out too), k, v [L, B, n_new, H, D]; rope, the weights, positions and lens_out may be None."""
     _cache_for(p, dst)
-    dev, rows, n_new = dst.device, _rows_dtype(p), k.shape[2]
-    HQ = p.n_kv_heads * p.group
-    qp, qs = _token_rows(q, p, HQ, n_new, rows, dev, "q") if q is not None else (None, 0)
-    kp, ks = _token_rows(k, p, p.n_kv_heads, n_new, rows, dev, "k")
-    vp, vs = _token_rows(v, p, p.n_kv_heads, n_new, rows, dev, "v")
-    x = NewTokens(qp, kp, vp, qs, ks, vs, _arg(q_weight, rows, p.head_dim, dev, "q_weight"),
-                  _arg(k_weight, rows, p.head_dim, dev, "k_weight"), norm_eps,
-                  _arg(positions, torch.int32, p.batch, dev, "positions"), n_new)
-    _launch(lib().ams_append, "ams_append", dev, stream, C.byref(p), C.byref(x), C.byref(rope) if rope is not None else None,
-            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"),
-            _arg(q_out, rows, p.n_layers * p.batch * HQ * n_new * p.head_dim, dev, "q_out"), C.byref(dst),
-            _arg(lens_out, torch.int32, p.batch, dev, "lens_out"))
+    L, batch, H, D, n_new = p.n_layers, p.batch, p.n_kv_heads, p.head_dim, k.shape[2]
+    dev, rows, HQ = dst.device, _ROWS[p.kv_dtype], H * p.group
+    qp, qs = _token_rows(q, (L, batch, n_new, HQ, D), rows, dev, "q") if q is not None else (None, 0)
+    kp, ks = _token_rows(k, (L, batch, n_new, H, D), rows, dev, "k")
+    vp, vs = _token_rows(v, (L, batch, n_new, H, D), rows, dev, "v")
+    x = NewTokens(qp, kp, vp, qs, ks, vs, _arg(q_weight, rows, D, dev, "q_weight"), _arg(k_weight, rows, D, dev, "k_weight"), norm_eps,
+                  _arg(positions, torch.int32, batch, dev, "positions"), n_new)
+    _launch((_lib or lib()).ams_append, "ams_append", dev, stream, C.byref(p), C.byref(x), C.byref(rope) if rope is not None else None,
+            _arg(seq_lens, torch.int32, batch, dev, "seq_lens"), _arg(q_out, rows, L * batch * HQ * n_new * D, dev, "q_out"), C.byref(dst),
+            _arg(lens_out, torch.int32, batch, dev, "lens_out"))
 
 
 def ams_attend_workspace_bytes(p: Params) -> int:
@@ -362,7 +361,7 @@ def ams_attend(p, src, seq_lens, q, out, ws, lse=None, weights_in=None, weights_
     _cache_for(p, src)
     dev, rows = src.device, _rows_dtype(p)
     n = p.units * p.group * p.window
-    _launch(lib().ams_attend, "ams_attend", dev, stream, C.byref(p), C.byref(src),
+    _launch((_lib or lib()).ams_attend, "ams_attend", dev, stream, C.byref(p), C.byref(src),
             _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"), _arg(q, rows, n * p.head_dim, dev, "q"),
             _arg(out, rows, n * p.head_dim, dev, "out"), _arg(lse, torch.float32, n, dev, "lse"),
             _arg(weights_in, torch.float32, p.units * p.t_stride, dev, "weights_in"),
@@ -376,7 +375,7 @@ def ams_recode(p, src, seq_lens, dst, idx=None, n_kept=None, credit_src=None, cr
     dev = src.device
     if dst.device != dev:
         raise ValueError("both caches lie on one GPU")
-    _launch(lib().ams_recode, "ams_recode", dev, stream, C.byref(p), C.byref(src),
+    _launch((_lib or lib()).ams_recode, "ams_recode", dev, stream, C.byref(p), C.byref(src),
             _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"), _arg(idx, torch.int32, p.units * p.budget, dev, "idx"),
             _arg(n_kept, torch.int32, p.units, dev, "n_kept"), C.byref(dst),
             _arg(credit_src, torch.float32, p.units * p.t_stride, dev, "credit_src"),
@@ -393,7 +392,7 @@ def ams_evict(p, src, seq_lens, weights, dst, weights_out, idx, n_kept, ws, lens
     dev = src.device
     if dst.device != dev:
         raise ValueError("both caches lie on one GPU")
-    _launch(lib().ams_evict, "ams_evict", dev, stream, C.byref(p), C.byref(src),
+    _launch((_lib or lib()).ams_evict, "ams_evict", dev, stream, C.byref(p), C.byref(src),
             _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"),
             _arg(weights, torch.float32, p.units * p.t_stride, dev, "weights"), C.byref(dst),
             _arg(weights_out, torch.float32, p.units * p.t_stride, dev, "weights_out"),

@@ -3,9 +3,12 @@
 //
 // A workgroup takes the new tokens that fall into one block of 16 positions of a sequence and a slice of the heads.  It
 // forms the cosines and sines of those tokens once, for all of its heads; a wave then takes a head at a time, eight channels a
-// lane (16 lanes a row of 128 channels, four rows a load), sums the squares over the row's lanes, finds the other channel of a pair
-// in LDS and writes.  The block is the unit because its rows share a scale: all of them are in the wave's registers when the
-// largest magnitude is known.
+// lane (16 lanes a row of 128 channels, four rows a load) and sums the squares over the row's lanes.  The block is the unit because its
+// rows share a scale: all of them are in the wave's registers when the largest magnitude is known.
+// A lane's eight channels are two runs of four, placed so that a pair's channels are in one lane (halves: 4 i and half + 4 i): no
+// exchange, and four cosines and sines in one LDS read each.  (Eight channels in a row, with the other halves and interleaved
+// cosines and sines out of LDS, took 35 us for 2036 tokens of 48 heads against 23: every read hit the same banks.)  Halves that are no
+// multiple of four channels find the other channel in LDS.
 // Angles: position * (frequency / 2 pi) in 64 bits, whole turns taken off there: at position 10^6 fp32 would be off by 0.06 rad.
 // Keys that go to 8 bits are normalised and rotated in 64 bits: a code changes by a whole step where the value
 // crosses the middle between two, and fp32 takes about one key element in a million across.
@@ -17,8 +20,9 @@ namespace {
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kPairs = 64;  // most rotated pairs
 
+enum { TURN_NONE = 0, TURN_HALVES = 1, TURN_NEIGHBOURS = 2, TURN_ANY_HALVES = 3 };
 struct Rotation {
-  int layout, rot_dim;
+  int mode, pairs;
   float gain;
   double turns[kPairs];  // per position
 };
@@ -33,42 +37,109 @@ __device__ __forceinline__ float round_to_odd(double y) {
   return __uint_as_float(u | 1u);
 }
 
+// Cosine and sine of t turns, |t| <= 1/2: the nearest quarter turn off, Taylor's polynomials on |r| <= pi / 4 (the first term left
+// out is 1e-15 of 1 in 64 bits; fp32 keeps 2e-9).
 template <typename M>
-struct Turn {
-  M cos, sin;
+__device__ __forceinline__ void cos_sin(double t, M& c, M& s) {
+  const double quarter = rint(4.0 * t);
+  const M r = (M)((t - 0.25 * quarter) * 6.283185307179586), z = r * r;
+  M pc, ps;
+  if constexpr (sizeof(M) == 8) {
+    ps = fma(z, fma(z, fma(z, fma(z, fma(z, fma(z, -1.0 / 1307674368000.0, 1.0 / 6227020800.0), -1.0 / 39916800.0), 1.0 / 362880.0), -1.0 / 5040.0),
+                    1.0 / 120.0), -1.0 / 6.0);
+    pc = fma(z, fma(z, fma(z, fma(z, fma(z, fma(z, fma(z, 1.0 / 20922789888000.0, -1.0 / 87178291200.0), 1.0 / 479001600.0), -1.0 / 3628800.0),
+                                  1.0 / 40320.0), -1.0 / 720.0), 1.0 / 24.0), -0.5);
+  } else {
+    ps = fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f);
+    pc = fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f);
+  }
+  const M sine = r + r * z * ps, cosine = (M)1 + z * pc;
+  const int q = (int)quarter & 3;
+  const M a = q & 1 ? sine : cosine, b = q & 1 ? cosine : sine;
+  c = (q == 1 || q == 2) ? -a : a;
+  s = (q >= 2) ? -b : b;
+}
+
+// Sum over the lanes of a row (16 or 8 of them).
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xF, 0xF, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int LANES, typename M>
+__device__ __forceinline__ M row_sum(M x) {
+  if constexpr (LANES == 16) x += moved<0x140>(x);  // lane 15 - i of 16
+  x += moved<0x141>(x);                             // 7 - i of 8
+  x += moved<0x4E>(x);                              // i ^ 2
+  return x + moved<0xB1>(x);                        // i ^ 1
+}
+__device__ __forceinline__ float inverse_root(float v) { return v < 0x1p-100f ? 1.f / sqrtf(v) : __builtin_amdgcn_rsqf(v); }
+__device__ __forceinline__ double inverse_root(double v) {
+  double y = __builtin_amdgcn_rsq(v);  // 2^-14 or better, doubled twice
+  if (v < 0x1p-1000 || !(y < 0x1p600)) return 1.0 / sqrt(v);
+  for (int i = 0; i < 2; ++i) y = fma(y, 0.5 * fma(-v * y, y, 1.0), y);
+  return y;
+}
+
+// Cosines and sines of a block's tokens.
+template <typename M>
+struct Turns {
+  __align__(16) M cos[kBlockRows][kPairs], sin[kBlockRows][kPairs];
 };
 
-// Norm and rotation of the wave's rows: eight channels 8 i .. 8 i + 7 of row x -> y.
-template <typename M, typename TAB, int HD>
+// First channels of the two runs of four that lane i of a row holds.
+__device__ __forceinline__ void lane_runs(const Rotation& rot, int i, int& a, int& b) {
+  a = 8 * i, b = 8 * i + 4;
+  if (rot.mode == TURN_HALVES) {
+    const int lanes = rot.pairs / 4;
+    if (i < lanes) a = 4 * i, b = rot.pairs + 4 * i;  // else behind the 8 lanes channels that rotate, in order
+  }
+}
+
+// Norm and rotation of the wave's rows: channels a .. a + 3 and b .. b + 3 of row x -> y.
+template <typename M, int HD>
 __device__ __forceinline__ void normed_and_turned(const float (&x)[8], const float (&weight)[8], bool norm, float eps, const Rotation& rot,
-                                                  const Turn<TAB>* row_turns, M* exchange, int i, M (&y)[8]) {
-  constexpr int LANES = HD / 8;
+                                                  const M* cos_row, const M* sin_row, M* exchange, int i, M (&y)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] = (M)x[e];
   if (norm) {
     M ss = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss += y[e] * y[e];
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
-    const M inverse = (M)1 / sqrt(ss / (M)HD + (M)eps);
+    for (int e = 0; e < 8; ++e) ss = fma(y[e], y[e], ss);
+    const M inverse = inverse_root(row_sum<HD / 8>(ss) * (M)(1.0 / HD) + (M)eps);
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] *= inverse * (M)weight[e];
   }
-  if (rot.rot_dim == 0) return;
-  if (rot.layout == AMS_ROPE_INTERLEAVED) {
+  if (rot.mode == TURN_NONE) return;
+  if (rot.mode != TURN_ANY_HALVES) {
+    M c[4], s[4];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const int d = 8 * i + e;
-      if (d >= rot.rot_dim) continue;
-      const M c = (M)row_turns[d / 2].cos, s = (M)row_turns[d / 2].sin;
-      const M p = y[e], q = y[e + 1];
-      y[e] = p * c - q * s;
-      y[e + 1] = q * c + p * s;
+    for (int e = 0; e < 4; ++e) {
+      c[e] = cos_row[4 * i + e], s[e] = sin_row[4 * i + e];
+      if (4 * i + e >= rot.pairs) c[e] = (M)1, s[e] = (M)0;
+    }
+    if (rot.mode == TURN_HALVES) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const M p = y[e], q = y[4 + e];
+        y[e] = p * c[e] - q * s[e], y[4 + e] = q * c[e] + p * s[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const M p = y[2 * e], q = y[2 * e + 1];
+        y[2 * e] = p * c[e] - q * s[e], y[2 * e + 1] = q * c[e] + p * s[e];
+      }
     }
     return;
   }
-  const int half = rot.rot_dim / 2;
+  const int half = rot.pairs;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own stretch of LDS: its last readers are done
 #pragma unroll
   for (int e = 0; e < 8; ++e) exchange[8 * i + e] = y[e];
@@ -77,24 +148,57 @@ __device__ __forceinline__ void normed_and_turned(const float (&x)[8], const flo
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int d = 8 * i + e;
-    if (d >= rot.rot_dim) continue;
+    if (d >= 2 * half) continue;
     const bool second = d >= half;
     const int pair = second ? d - half : d;
-    const M c = (M)row_turns[pair].cos, s = (M)row_turns[pair].sin;
-    const M other = exchange[second ? pair : d + half];
+    const M c = cos_row[pair], s = sin_row[pair], other = exchange[second ? pair : d + half];
     y[e] = second ? y[e] * c + other * s : y[e] * c - other * s;
   }
   __builtin_amdgcn_wave_barrier();
 }
 
+// Two runs of four elements of a row.
+template <int EL>
+__device__ __forceinline__ void load_runs(const char* row, int a, int b, float (&x)[8]) {
+  if constexpr (EL == EL_F32) {
+    const float4 p = *(const float4*)(row + a * 4), q = *(const float4*)(row + b * 4);
+    x[0] = p.x, x[1] = p.y, x[2] = p.z, x[3] = p.w, x[4] = q.x, x[5] = q.y, x[6] = q.z, x[7] = q.w;
+  } else if constexpr (EL == EL_BF16) {
+    const uint2 p = *(const uint2*)(row + a * 2), q = *(const uint2*)(row + b * 2);
+    const uint32_t w[4] = {p.x, p.y, q.x, q.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  } else {
+    float lo[4], hi[4];
+    unpack_codes<EL>(*(const uint32_t*)(row + a), lo);
+    unpack_codes<EL>(*(const uint32_t*)(row + b), hi);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = lo[i], x[4 + i] = hi[i];
+  }
+}
+template <int EL>
+__device__ __forceinline__ void store_runs(char* row, int a, int b, const float (&x)[8], float inverse = 1.f) {
+  if constexpr (EL == EL_F32) {
+    *(float4*)(row + a * 4) = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4*)(row + b * 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else if constexpr (EL == EL_BF16) {
+    *(uint2*)(row + a * 2) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
+    *(uint2*)(row + b * 2) = make_uint2(bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+  } else {
+    const uint2 p = pack_eight<EL>(x, inverse);
+    *(uint32_t*)(row + a) = p.x, *(uint32_t*)(row + b) = p.y;
+  }
+}
+
 // DST: element type of the cache; BF16: of the new rows (and of a cache of kv_dtype).
 template <int DST, bool BF16, int HD>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation rot, int tasks_per_group) {
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation rot) {
   constexpr int SRC = BF16 ? EL_BF16 : EL_F32, ES = kElBytes<SRC>;
   constexpr int LANES = HD / 8, ROWS = 64 / LANES, PASSES = kBlockRows / ROWS;
   constexpr bool PACK = kPacked<DST>;
-  using M = std::conditional_t<PACK, double, float>;  // of keys, and of the table
-  __shared__ Turn<M> turns[kBlockRows][kPairs];
+  using M = std::conditional_t<PACK, double, float>;  // of keys
+  __shared__ Turns<float> turns;
+  __shared__ Turns<M> exact;  // (unused where M is float)
   __shared__ __align__(16) M exchange[kWaves][ROWS][HD];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int b = blockIdx.y % a.d.B, l = blockIdx.y / a.d.B;
@@ -105,51 +209,55 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
     a.lens_out[b] = min(len + a.n_new, a.d.t_max);
   const int count = hi - lo, kept = min(hi, a.d.t_max) - lo;  // tokens here; those that the cache takes
   if (count <= 0) return;
-  const int first = a.positions ? a.positions[b] : len;
-  const int pairs = rot.rot_dim / 2;
-  for (int k = threadIdx.x; k < count * pairs; k += kThreads) {
-    const int r = k / pairs, i = k % pairs;
-    double t = ((double)first + (double)(lo - len + r)) * rot.turns[i];
-    t -= rint(t);
-    M s, c;
-    if constexpr (PACK) {
-      sincospi(2.0 * t, &s, &c);
-    } else {
-      sincospif((float)(2.0 * t), &s, &c);
-    }
-    turns[r][i] = Turn<M>{c * (M)rot.gain, s * (M)rot.gain};
-  }
-  __syncthreads();
   const int H = a.d.H, HQ = a.q ? H * a.d.G : 0, n_tasks = HQ + 2 * H;
   const int i = lane % LANES, r0 = lane / LANES;
-  float qw[8], kw[8];
-  if (a.q_weight) load_eight<SRC>(a.q_weight + i * 8 * ES, qw);
-  if (a.k_weight) load_eight<SRC>(a.k_weight + i * 8 * ES, kw);
+  int run_a, run_b;
+  lane_runs(rot, i, run_a, run_b);
   const int64_t token0 = ((int64_t)l * a.d.B + b) * a.n_new + (lo - len);
-  const int end = min(n_tasks, (int)(blockIdx.z + 1) * tasks_per_group);
-  for (int task = blockIdx.z * tasks_per_group + wave; task < end; task += kWaves) {
+  // the rows of a head's task: queries, then keys, then values
+  float x[PASSES][8];
+  auto fetch = [&](int task) __attribute__((always_inline)) {
     const bool is_q = task < HQ, is_k = !is_q && task < HQ + H;
     const int head = is_q ? task : is_k ? task - HQ : task - HQ - H;
-    const char* src = (is_q ? a.q + token0 * a.q_stride : is_k ? a.k + token0 * a.k_stride : a.v + token0 * a.v_stride) +
-                      (int64_t)head * HD * ES + i * 8 * ES;
     const int64_t step = is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride;
-    float x[PASSES][8];
+    const char* src = (is_q ? a.q : is_k ? a.k : a.v) + token0 * step + (int64_t)head * HD * ES;
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-      const int r = p * ROWS + r0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[p][e] = 0.f;
-      if (r < count) load_eight<SRC>(src + r * step, x[p]);
+      if (p * ROWS >= count) break;
+      load_runs<SRC>(src + min(p * ROWS + r0, count - 1) * step, run_a, run_b, x[p]);  // (rows past the last are that one again)
     }
+  };
+  int task = wave * gridDim.z + blockIdx.z;  // every workgroup has its share of the keys, which take longest
+  const int task_step = kWaves * gridDim.z;
+  if (task < n_tasks) fetch(task);  // on its way while the angles are formed
+  const int first = a.positions ? a.positions[b] : len;
+  for (int k = threadIdx.x; k < count * kPairs; k += kThreads) {
+    const int r = k / kPairs, pair = k % kPairs;
+    if (pair >= rot.pairs) continue;
+    double t = ((double)first + (double)(lo - len + r)) * rot.turns[pair];
+    t -= rint(t);
+    M s, c;
+    cos_sin(t, c, s);
+    c *= (M)rot.gain, s *= (M)rot.gain;
+    turns.cos[r][pair] = (float)c, turns.sin[r][pair] = (float)s;
+    if constexpr (PACK) exact.cos[r][pair] = c, exact.sin[r][pair] = s;
+  }
+  __syncthreads();
+  for (; task < n_tasks; task += task_step, task < n_tasks ? fetch(task) : (void)0) {
+    const bool is_q = task < HQ, is_k = !is_q && task < HQ + H;
+    const int head = is_q ? task : is_k ? task - HQ : task - HQ - H;
+    float weight[8];
+    const char* given = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
+    if (given) load_runs<SRC>(given, run_a, run_b, weight);
     if (is_q) {
-      char* to = a.q_out + ((((int64_t)l * a.d.B + b) * HQ + head) * a.n_new + (lo - len)) * (HD * ES) + i * 8 * ES;
+      char* to = a.q_out + ((((int64_t)l * a.d.B + b) * HQ + head) * a.n_new + (lo - len)) * (HD * ES);
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
         if (p * ROWS >= count) break;
         const int r = p * ROWS + r0;
         float y[8];
-        normed_and_turned<float, M, HD>(x[p], qw, a.q_weight != nullptr, a.eps, rot, turns[r], (float*)exchange[wave][r0], i, y);
-        if (r < count) store_eight<SRC>(to + r * (HD * ES), y);
+        normed_and_turned<float, HD>(x[p], weight, given != nullptr, a.eps, rot, turns.cos[r], turns.sin[r], (float*)exchange[wave][r0], i, y);
+        if (r < count) store_runs<SRC>(to + r * (HD * ES), run_a, run_b, y);
       }
       continue;
     }
@@ -159,7 +267,13 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
       for (int p = 0; p < PASSES; ++p) {
         if (p * ROWS >= count) break;
         M y[8];
-        normed_and_turned<M, M, HD>(x[p], kw, a.k_weight != nullptr, a.eps, rot, turns[p * ROWS + r0], exchange[wave][r0], i, y);
+        const int r = p * ROWS + r0;
+        const M *cos_row, *sin_row;
+        if constexpr (PACK)
+          cos_row = exact.cos[r], sin_row = exact.sin[r];
+        else
+          cos_row = turns.cos[r], sin_row = turns.sin[r];
+        normed_and_turned<M, HD>(x[p], weight, given != nullptr, a.eps, rot, cos_row, sin_row, exchange[wave][r0], i, y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           if constexpr (PACK)
@@ -177,13 +291,13 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
         const int r = p * ROWS + r0;
-        if (r < kept) store_eight<SRC>(to.row0 + (old + r) * to.stride + i * 8 * ES, x[p]);
+        if (r < kept) store_runs<SRC>(to.row0 + (old + r) * to.stride, run_a, run_b, x[p]);
       }
     } else {
       uint32_t top = 0;
 #pragma unroll
       for (int p = 0; p < PASSES; ++p)
-        if (p * ROWS + r0 < kept) top = top_bits(x[p], top);
+        if (p * ROWS + r0 < kept) top = top_bits(x[p], top);  // (not those past t_max)
       const float need = block_scale<DST>(wave_max(top)), had = old > 0 ? dst.scale[to.scale] : 0.f;
       const bool number = need == need && had == had;
       const float scale = number ? fmaxf(need, had) : __uint_as_float(0x7FC00000u);
@@ -194,17 +308,17 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
         for (int p = 0; p < PASSES; ++p) {
           const int r = p * ROWS + r0;
           if (r < old) {
-            char* at = to.row0 + r * to.stride + i * 8;
+            char* at = to.row0 + r * to.stride;
             float y[8];
-            load_eight<DST>(at, y);
-            *(uint2*)at = pack_eight<DST>(y, ratio);
+            load_runs<DST>(at, run_a, run_b, y);
+            store_runs<DST>(at, run_a, run_b, y, ratio);
           }
         }
       }
 #pragma unroll
       for (int p = 0; p < PASSES; ++p) {
         const int r = p * ROWS + r0;
-        if (r < kept) *(uint2*)(to.row0 + (old + r) * to.stride + i * 8) = pack_eight<DST>(x[p], inverse);
+        if (r < kept) store_runs<DST>(to.row0 + (old + r) * to.stride, run_a, run_b, x[p], inverse);
       }
       if (lane == 0 && (old == 0 || !(scale == had))) dst.scale[to.scale] = scale;
     }
@@ -215,10 +329,12 @@ template <int DST, bool BF16, int HD>
 hipError_t launch(const AppendArgs& a, const Rotation& rot, hipStream_t s) {
   const int tiles = (a.n_new + 14) / kBlockRows + 1, rows = a.d.L * a.d.B;
   const int tasks = (a.q ? a.d.H * a.d.G : 0) + 2 * a.d.H;
-  int per = kWaves;
-  while (per < tasks && (int64_t)tiles * rows * div_up(tasks, per) > 2048) per *= 2;
+  // Slices of the heads: one round of workgroups, two on a CU where keys are formed in 64 bits (their registers), else four.  2036
+  // tokens of 48 heads to 8 bits: 19.9 us with 396 workgroups, 24.9 with 792, 29.8 with 1584; 4096 tokens, bf16: 39.6 with 258,
+  // 25.8 with 774, 29.4 with 1548.
+  const int slices = min(max(1, (kPacked<DST> ? 512 : 1024) / (int)min((int64_t)tiles * rows, (int64_t)1024)), div_up(tasks, kWaves));
   prof_mark("append", s);
-  hipLaunchKernelGGL((append_kernel<DST, BF16, HD>), dim3(tiles, rows, div_up(tasks, per)), dim3(kThreads), 0, s, a, rot, per);
+  hipLaunchKernelGGL((append_kernel<DST, BF16, HD>), dim3(tiles, rows, slices), dim3(kThreads), 0, s, a, rot);
   return hipGetLastError();
 }
 
@@ -236,8 +352,9 @@ hipError_t launch_to(const AppendArgs& a, const Rotation& rot, int el, hipStream
 hipError_t launch_append(const AppendArgs& a, const ams_rope* rope, bool bf16, int dst_el, hipStream_t s) {
   Rotation rot{};
   if (rope) {
-    rot.layout = rope->layout, rot.rot_dim = rope->rot_dim, rot.gain = rope->gain;
-    for (int i = 0; i < rope->rot_dim / 2; ++i) rot.turns[i] = rope->freq[i] / 6.283185307179586;
+    rot.pairs = rope->rot_dim / 2, rot.gain = rope->gain;
+    rot.mode = rot.pairs == 0 ? TURN_NONE : rope->layout == AMS_ROPE_INTERLEAVED ? TURN_NEIGHBOURS : rot.pairs % 4 ? TURN_ANY_HALVES : TURN_HALVES;
+    for (int i = 0; i < rot.pairs; ++i) rot.turns[i] = rope->freq[i] / 6.283185307179586;
   }
   if (a.d.D == 128) return bf16 ? launch_to<true, 128>(a, rot, dst_el, s) : launch_to<false, 128>(a, rot, dst_el, s);
   return bf16 ? launch_to<true, 64>(a, rot, dst_el, s) : launch_to<false, 64>(a, rot, dst_el, s);
