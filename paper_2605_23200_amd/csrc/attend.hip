@@ -83,6 +83,25 @@ __device__ __forceinline__ float query_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// Over the sixteen lanes that hold one position's logits.
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float sixteen_sum(float x) {
+  x += moved<0x140>(x);         // lane 15 - i of 16
+  x += moved<0x141>(x);         // 7 - i of 8
+  x += moved<0x4E>(x);          // i ^ 2
+  return x + moved<0xB1>(x);    // i ^ 1
+}
+
+__device__ __forceinline__ float sixteen_max(float x) {
+  x = fmaxf(x, moved<0x140>(x));
+  x = fmaxf(x, moved<0x141>(x));
+  x = fmaxf(x, moved<0x4E>(x));
+  return fmaxf(x, moved<0xB1>(x));
+}
+
 // Channel of element 0 of the 8 that lane group g feeds to product i of q.k: 16 bytes of a K row per load.
 __device__ __forceinline__ int k_channel(int i, int g) { return 64 * (i >> 1) + 16 * g + 8 * (i & 1); }
 
@@ -92,27 +111,25 @@ struct Queries {
   static constexpr int TERMS = BF16 ? 1 : 3, STEPS = HD / 32;
   bf16x8 x[R][STEPS][TERMS];
   __device__ __forceinline__ void load(const char* unit_q, int row0, int N, int lane) {
-    const int g = lane >> 4;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int n = row0 + r * 16 + (lane & 15);
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int d = k_channel(i, g);
-        if constexpr (BF16) {
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (n < N) v = *(const uint4*)(unit_q + ((int64_t)n * HD + d) * 2);
-          x[r][i][0] = __builtin_bit_cast(bf16x8, v);
-        } else {
-          float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-          if (n < N) load_eight<EL_F32>(unit_q + ((int64_t)n * HD + d) * 4, v);
-          uint32_t t[3][4];
+      for (int i = 0; i < STEPS; ++i) load_one(unit_q, row0 + r * 16 + (lane & 15), N, i, lane, x[r][i]);
+  }
+  static __device__ __forceinline__ void load_one(const char* unit_q, int n, int N, int i, int lane, bf16x8 (&out)[TERMS]) {
+    const int d = k_channel(i, lane >> 4);
+    if constexpr (BF16) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (n < N) v = *(const uint4*)(unit_q + ((int64_t)n * HD + d) * 2);
+      out[0] = __builtin_bit_cast(bf16x8, v);
+    } else {
+      float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (n < N) load_eight<EL_F32>(unit_q + ((int64_t)n * HD + d) * 4, v);
+      uint32_t t[3][4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) split2<true>(v[2 * j], v[2 * j + 1], t[0][j], t[1][j], t[2][j]);
+      for (int j = 0; j < 4; ++j) split2<true>(v[2 * j], v[2 * j + 1], t[0][j], t[1][j], t[2][j]);
 #pragma unroll
-          for (int k = 0; k < 3; ++k) x[r][i][k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]));
-        }
-      }
+      for (int k = 0; k < 3; ++k) out[k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0], t[k][1], t[k][2], t[k][3]));
     }
   }
 };
@@ -214,16 +231,19 @@ struct VTile {
   }
 };
 
-// One split of one unit's positions for 16 R of its queries.
+// One split of one unit's positions for 16 R row_waves of its queries: row_waves waves side by side take 16 R queries each, the others
+// every (4 / row_waves)-th step of the positions.
 template <int EL, bool BF16, int HD, int R>
-__global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF16 || HD == 64 ? 2 : 1)) void attend_kernel(AttendArgs a) {
   constexpr int STEPS = HD / 32, TILES = HD / 16, TERMS = BF16 ? 1 : 3, PTERMS = BF16 ? 2 : 3;
   constexpr int LD = HD + 4;  // row of the join in LDS
   __shared__ __align__(16) float joint[kWaves][16][LD];
   __shared__ float2 stat[kWaves][16];
-  const int unit = blockIdx.y, split = blockIdx.x, row0 = blockIdx.z * 16 * R;
+  const int unit = blockIdx.y, split = blockIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 4, c = lane & 15;
+  const int row_waves = a.row_waves, key_waves = kWaves / row_waves, stride = key_waves * kStep;
+  const int row0 = (blockIdx.z * row_waves + wave % row_waves) * 16 * R;
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b), N = a.d.N;
@@ -268,11 +288,12 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) 
       off.set(u.row_stride, lane, min(T - 1 - at, kBlockRows - 1), T - 1 - blk1 * kBlockRows);
     }
   };
-  int at = begin + wave * kStep;
+  int at = begin + wave / row_waves * kStep;
   // One step.  MORE: there is another, whose K is loaded when this one's has been used, V likewise.  (Loads under a condition that
   // the compiler cannot follow would make every wait one for all loads.)
   auto step = [&](auto more) __attribute__((always_inline)) {
     constexpr bool MORE = decltype(more)::value;
+    const bool whole = at + kStep <= fewest;  // every query sees every position of the step
     floatx4 s[2][R];
     float kscale[2];
 #pragma unroll
@@ -289,25 +310,27 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) 
           for (int t = TERMS - 1; t >= 0; --t) s[j][r] = mma(k, q.x[r][i][t], s[j][r]);
       }
     }
-    const int next = at + kWaves * kStep;
+    const int next = at + stride;
     if constexpr (MORE) {
       settle(next);
       kt[0].load(u, slot[0], off.k[0]);
       kt[1].load(u, slot[1], off.k[1]);
-      find(next + kWaves * kStep);
+      find(next + stride);
     }
-    const bool whole = at + kStep <= fewest;  // every query sees every position of the step
     bf16x8 p[R][PTERMS];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float x[8];
       float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[j] = s[j >> 2][r][j & 3] * kscale[j >> 2];
-        if (!whole && at + (j >> 2) * 16 + 4 * g + (j & 3) >= limit[r]) x[j] = -INFINITY;
-        top = fmaxf(top, x[j]);
+      for (int j = 0; j < 8; ++j) x[j] = s[j >> 2][r][j & 3] * kscale[j >> 2];
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (at + (j >> 2) * 16 + 4 * g + (j & 3) >= limit[r]) x[j] = -INFINITY;
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
       if (__any(top > m[r] + kSlack)) {
         const float now = fmaxf(m[r], query_max(top)), shrink = power_of_two(m[r] - now);
         m[r] = now;
@@ -355,22 +378,20 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) 
     }
     if constexpr (MORE) vt.load(u, slot[0], slot[1], off);
   };
-  if (at < end) {
+  if (at < end && row0 < N) {
     find(at);
     settle(at);
     kt[0].load(u, slot[0], off.k[0]);
     kt[1].load(u, slot[1], off.k[1]);
     vt.load(u, slot[0], slot[1], off);
-    find(at + kWaves * kStep);
-    for (; at + kWaves * kStep < end; at += kWaves * kStep) step(std::true_type{});
+    find(at + stride);
+    for (; at + stride < end; at += stride) step(std::true_type{});
     step(std::false_type{});
   }
-  // the four waves together: 16 queries at a time, thread (query, stretch of HD / 16 channels)
+  // the waves of the same queries together: 16 queries at a time, thread (query, stretch of HD / 16 channels)
   const bool last = a.n_splits == 1;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int n0 = row0 + r * 16;
-    if (n0 >= N) break;
     if (r > 0) __syncthreads();
     const float total = query_sum(sum[r]);
     if (g == 0) stat[wave][c] = make_float2(m[r], total);
@@ -380,21 +401,21 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : 1) 
       for (int e = 0; e < TILES; e += 4)
         *(float4*)&joint[wave][c][TILES * (4 * g + q4) + e] = make_float4(o[r][e][q4], o[r][e + 1][q4], o[r][e + 2][q4], o[r][e + 3][q4]);
     __syncthreads();
-    const int qr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * TILES, n = n0 + qr;
-    float top = stat[0][qr].x;
+    const int qr = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * TILES;
+    for (int q = 0; q < row_waves; ++q) {
+      const int n = (blockIdx.z * row_waves + q) * 16 * R + r * 16 + qr;
+      if (n >= N) continue;
+      float top = stat[q][qr].x;
+      for (int w = q + row_waves; w < kWaves; w += row_waves) top = fmaxf(top, stat[w][qr].x);
+      float x[TILES], all = 0.f;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, stat[w][qr].x);
-    float x[TILES], all = 0.f;
+      for (int e = 0; e < TILES; ++e) x[e] = 0.f;
+      for (int w = q; w < kWaves; w += row_waves) {
+        const float f = power_of_two(stat[w][qr].x - top);
+        all = fmaf(f, stat[w][qr].y, all);
 #pragma unroll
-    for (int e = 0; e < TILES; ++e) x[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = power_of_two(stat[w][qr].x - top);
-      all += f * stat[w][qr].y;
-#pragma unroll
-      for (int e = 0; e < TILES; ++e) x[e] = fmaf(f, joint[w][qr][d0 + e], x[e]);
-    }
-    if (n < N) {
+        for (int e = 0; e < TILES; ++e) x[e] = fmaf(f, joint[w][qr][d0 + e], x[e]);
+      }
       const int64_t row = ((int64_t)unit * a.n_splits + split) * N + n;
       if (threadIdx.x % 16 == 0) {
         a.stats[((int64_t)unit * N + n) * a.n_splits + split] = make_float2(top, all);
@@ -494,7 +515,7 @@ constexpr int kStashKeys = 4 * kThreads;  // positions per workgroup that turns 
 template <bool BF16, int HD>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int joins) {
   __shared__ float2 stat[16];
-  const int unit = blockIdx.y, lane = threadIdx.x & 63, N = a.d.N;
+  const int unit = blockIdx.y, N = a.d.N;
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b), splits = splits_of(a, T);
@@ -504,9 +525,17 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
   }
   const int first = ((int)blockIdx.x - joins) * kStashKeys;
   if (first >= T) return;
-  for (int n = threadIdx.x >> 6; n < N; n += kWaves) {
-    const float2 st = joined_stats(a, unit, n, splits, lane);
-    if (lane == 0) stat[n] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
+  {  // sixteen lanes a query
+    const int n = threadIdx.x >> 4, c = threadIdx.x & 15;
+    const float2* at = a.stats + ((int64_t)unit * N + min(n, N - 1)) * a.n_splits;
+    float2 mine = make_float2(kLowest, 0.f);
+    for (int s = c; s < splits; s += 16) {
+      const float2 x = at[s];
+      const float top = fmaxf(mine.x, x.x);
+      mine = make_float2(top, mine.y * power_of_two(mine.x - top) + x.y * power_of_two(x.x - top));
+    }
+    const float top = sixteen_max(mine.x), sum = sixteen_sum(mine.y * power_of_two(mine.x - top));
+    if (c == 0) stat[n] = make_float2(top, sum == 0.f ? 0.f : 1.f / sum);
   }
   __syncthreads();
   const int t = first + 4 * threadIdx.x;
@@ -526,12 +555,19 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
     if (t + i < T) a.weights_out[at + i] = (a.weights_in ? a.weights_in[at + i] : 0.f) + w[i];
 }
 
-constexpr int kWeightKeys = kThreads;  // positions per workgroup of the kernel below
+// Weights from K again, for more queries than the stash is for.  The queries' operands of the whole call lie in LDS; a wave takes 64
+// positions at a time, converts them once, runs 32 queries at a time over them, and has the next 64 on their way.  (One step per
+// workgroup, with the queries loaded for it, is latency: 172 us for 64 units of 32768 positions and 32 queries, @@ with several.)
+constexpr int kWeightRows = 32, kWeightBlocks = 4, kWeightStep = kWaves * kWeightBlocks * kBlockRows;
+template <bool BF16, int HD>
+constexpr int kWeightGroupBytes = kWeightRows / 16 * (HD / 32) * (BF16 ? 1 : 3) * 64 * 16;
 
-// weights from K again: a wave takes 64 positions, 64 queries at a time.
 template <int EL, bool BF16, int HD>
-__global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a) {
-  constexpr int R = 4, STEPS = HD / 32, TERMS = BF16 ? 1 : 3, BLOCKS = 4;
+__global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, int row_begin, int row_end, int steps) {
+  constexpr int R = kWeightRows / 16, STEPS = HD / 32, TERMS = BF16 ? 1 : 3, BLOCKS = kWeightBlocks;
+  typedef bf16x8 Group[R][STEPS][TERMS][64];
+  extern __shared__ __align__(16) char lds[];
+  Group* q = (Group*)lds;
   __shared__ float2 stat[256];
   const int unit = blockIdx.y, N = a.d.N;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -539,69 +575,114 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a) 
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b);
-  if (blockIdx.x * kWeightKeys >= T) return;
-  if ((int)threadIdx.x < N) {  // joined, or of the only split
-    const float2 st = a.joined[(int64_t)unit * N + threadIdx.x];
-    stat[threadIdx.x] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
-  }
-  __syncthreads();
-  const int first = blockIdx.x * kWeightKeys + wave * 16 * BLOCKS;
-  if (first >= T) return;
-  const float to_log2 = kLog2E / sqrtf((float)HD);
+  const int start = blockIdx.x * steps * kWeightStep;
+  if (start >= T) return;
+  const int groups = (row_end - row_begin + kWeightRows - 1) / kWeightRows, last_blk = (T - 1) / kBlockRows;
   const UnitBlocks u(a.k, a.v, l, b, h);
   KTile<HD> k[BLOCKS];
-#pragma unroll
-  for (int j = 0; j < BLOCKS; ++j) {
-    const int blk = min(first / kBlockRows + j, (T - 1) / kBlockRows);
-    k[j].load(u, u.slot(u.named(blk)), (uint32_t)min(lane & 15, T - 1 - blk * kBlockRows) * u.row_stride + (lane >> 4) * 16);
-  }
-  float w[BLOCKS][4];
-#pragma unroll
-  for (int j = 0; j < BLOCKS; ++j) w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0.f;
-  for (int row0 = 0; row0 < N; row0 += 16 * R) {
-    Queries<BF16, HD, R> q;
-    q.load(a.q + (int64_t)unit * N * HD * (BF16 ? 2 : 4), row0, N, lane);
+  auto fetch = [&](int first) __attribute__((always_inline)) {  // (positions past the last: that one again)
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j) {
-      floatx4 s[R];
+      const int blk = min(first / kBlockRows + j, last_blk);
+      k[j].load(u, u.slot(u.named(blk)), (uint32_t)min(lane & 15, T - 1 - blk * kBlockRows) * u.row_stride + (lane >> 4) * 16);
+    }
+  };
+  int first = start + wave * BLOCKS * kBlockRows;
+  fetch(first);
+  {  // joined, or of the only split; a query that is not there counts nothing
+    const int n = row_begin + threadIdx.x;
+    const float2 st = n < row_end ? a.joined[(int64_t)unit * N + n] : make_float2(0.f, 0.f);
+    stat[threadIdx.x] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
+  }
+  const char* unit_q = a.q + (int64_t)unit * N * HD * (BF16 ? 2 : 4);
+  for (int f = wave; f < groups * R * STEPS; f += kWaves) {
+    const int group = f / (R * STEPS), r = f / STEPS % R, i = f % STEPS;
+    bf16x8 one[TERMS];
+    Queries<BF16, HD, R>::load_one(unit_q, row_begin + group * kWeightRows + r * 16 + c, row_end, i, lane, one);
 #pragma unroll
-      for (int r = 0; r < R; ++r) s[r] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < TERMS; ++t) q[group][r][i][t][lane] = one[t];
+  }
+  __syncthreads();
+  const float to_log2 = kLog2E / sqrtf((float)HD);
+  const int fewest = a.causal ? T - a.d.W + 1 : T;  // positions that every query sees
+  for (int step = 0; step < steps && first < T; ++step, first += kWeightStep) {
+    bf16x8 x[BLOCKS][STEPS];
+    float scale[BLOCKS], w[BLOCKS][4];
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const bf16x8 x = k[j].template operand<EL>(i);
+    for (int j = 0; j < BLOCKS; ++j) {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) x[j][i] = k[j].template operand<EL>(i);
+      scale[j] = k[j].scale * to_log2;
+      w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0.f;
+    }
+    fetch(first + kWeightStep);
+    const bool whole = first + BLOCKS * kBlockRows <= fewest;
+    for (int group = 0; group < groups; ++group) {
+      floatx4 s[BLOCKS][R];
+#pragma unroll
+      for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[j][r] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i)
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int t = TERMS - 1; t >= 0; --t) s[r] = mma(x, q.x[r][i][t], s[r]);
-      }
-      const float scale = k[j].scale * to_log2;
+          for (int t = TERMS - 1; t >= 0; --t) {
+            const bf16x8 y = q[group][r][i][t][lane];
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j) s[j][r] = mma(x[j][i], y, s[j][r]);
+          }
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const int n = row0 + r * 16 + c;
-        if (n >= N) continue;
-        const float2 st = stat[n];
-        const int limit = a.causal ? T - a.d.W + 1 + n % a.d.W : T;
+        const int m = group * kWeightRows + r * 16 + c, n = row_begin + m;
+        const float2 st = stat[m];
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = power_of_two(s[r][i] * scale - st.x) * st.y;
-          if (first + 16 * j + 4 * g + i < limit) w[j][i] += p;
+          for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[j][i] = fmaf(power_of_two(fmaf(s[j][r][i], scale[j], -st.x)), st.y, w[j][i]);
+        } else {
+          const int limit = n >= row_end ? 0 : a.causal ? T - a.d.W + 1 + n % a.d.W : T;
+#pragma unroll
+          for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float p = power_of_two(fmaf(s[j][r][i], scale[j], -st.x)) * st.y;
+              if (first + 16 * j + 4 * g + i < limit) w[j][i] += p;
+            }
         }
       }
     }
-  }
 #pragma unroll
-  for (int j = 0; j < BLOCKS; ++j) {
+    for (int j = 0; j < BLOCKS; ++j) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) w[j][i] += __shfl_xor(w[j][i], o);
-    const int t = first + 16 * j + 4 * g + (c & 3);
-    if (c < 4 && t < T) {
-      const int64_t at = (int64_t)unit * a.d.t_stride + t;
-      const float x = c == 0 ? w[j][0] : c == 1 ? w[j][1] : c == 2 ? w[j][2] : w[j][3];
-      a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + x;
+      for (int i = 0; i < 4; ++i) w[j][i] = sixteen_sum(w[j][i]);
+      const int t = first + 16 * j + 4 * g + (c & 3);
+      if (c < 4 && t < T) {
+        const int64_t at = (int64_t)unit * a.d.t_stride + t;
+        const float more = c == 0 ? w[j][0] : c == 1 ? w[j][1] : c == 2 ? w[j][2] : w[j][3];
+        a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + more;
+      }
     }
   }
+}
+
+template <int EL, bool BF16, int HD>
+hipError_t launch_weights(AttendArgs a, hipStream_t s) {
+  constexpr int kMost = 96 * 1024 / kWeightGroupBytes<BF16, HD> * kWeightRows;  // queries whose operands fit LDS (fp32, 128 channels: 128)
+  for (int row = 0; row < a.d.N; row += kMost) {
+    const int end = min(a.d.N, row + kMost), bytes = div_up(end - row, kWeightRows) * kWeightGroupBytes<BF16, HD>;
+    // steps per workgroup: one round of workgroups, two on a CU, where there are more
+    const int total = div_up(a.d.t_max, kWeightStep), steps = max(1, (int)((int64_t)total * a.d.units / 512));
+    hipError_t e = ensure_lds<attend_weights_kernel<EL, BF16, HD>>(bytes);
+    if (e != hipSuccess) return e;
+    prof_mark("attend_weights", s);
+    hipLaunchKernelGGL((attend_weights_kernel<EL, BF16, HD>), dim3(div_up(total, steps), a.d.units), dim3(kThreads), bytes, s, a, row, end,
+                       steps);
+    a.weights_in = a.weights_out;  // the next queries' are added
+  }
+  return hipSuccess;
 }
 
 template <int EL, bool BF16, int HD>
@@ -610,18 +691,16 @@ hipError_t launch(const AttendArgs& a, const AttendLayout& lay, hipStream_t s) {
   prof_mark("attend", s);
   if (lay.row_tiles == 1)
     hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 1>), grid, dim3(kThreads), 0, s, a);
-  else if (lay.row_tiles == 2)
-    hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 2>), grid, dim3(kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 4>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((attend_kernel<EL, BF16, HD, 2>), grid, dim3(kThreads), 0, s, a);
   const int joins = lay.n_splits > 1 ? a.d.N : 0, stash = a.stash ? div_up(a.d.t_max, kStashKeys) : 0;
   if (joins + stash > 0) {
     prof_mark("attend_join", s);
     hipLaunchKernelGGL((attend_join_kernel<BF16, HD>), dim3(joins + stash, a.d.units), dim3(kThreads), 0, s, a, joins);
   }
   if (a.weights_out && !a.stash) {
-    prof_mark("attend_weights", s);
-    hipLaunchKernelGGL((attend_weights_kernel<EL, BF16, HD>), dim3(div_up(a.d.t_max, kWeightKeys), a.d.units), dim3(kThreads), 0, s, a);
+    const hipError_t e = launch_weights<EL, BF16, HD>(a, s);
+    if (e != hipSuccess) return e;
   }
   return hipGetLastError();
 }
@@ -637,8 +716,9 @@ AttendLayout attend_layout(const ams_params* p) {
   AttendLayout r;
   const size_t units = (size_t)p->n_layers * p->batch * p->n_kv_heads, N = (size_t)p->group * p->window;
   const int tiles = div_up(N, 16);
-  r.row_tiles = tiles <= 1 ? 1 : tiles <= 2 ? 2 : 4;
-  r.row_groups = div_up(tiles, r.row_tiles);
+  r.row_tiles = tiles <= 1 ? 1 : 2;
+  r.row_waves = tiles <= 2 ? 1 : tiles <= 4 ? 2 : 4;
+  r.row_groups = div_up(tiles, r.row_tiles * r.row_waves);
   r.stashed = N <= 16;
   // Positions per workgroup: 512 where that fills the chip several times over (ragged sequences end at different times), else
   // as many as give one round of workgroups, three on a CU.
@@ -647,7 +727,7 @@ AttendLayout attend_layout(const ams_params* p) {
   if (fine >= 2048) {
     r.chunk = 512;
   } else {
-    const int splits = (int)max((size_t)1, (size_t)768 / per_split);
+    const int splits = (int)max((size_t)1, (size_t)(r.row_tiles == 1 ? 768 : 512) / per_split);
     r.chunk = div_up(div_up(p->t_max, splits), kWaves * kStep) * kWaves * kStep;
   }
   while (div_up(p->t_max, r.chunk) > 4096) r.chunk *= 2;  // what the join goes through

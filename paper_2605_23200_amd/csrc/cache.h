@@ -157,7 +157,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 // Where scratch of ams_attend lies.
 struct AttendLayout {
   size_t part, stats, joined, stash, total;  // outputs and statistics of the splits, logits
-  int chunk, n_splits, row_tiles, row_groups;
+  int chunk, n_splits, row_tiles, row_waves, row_groups;
   bool stashed;  // the logits are kept for the weights
 };
 
@@ -190,7 +190,7 @@ struct AttendArgs {
   float2* stats;  // [units, N, splits]: largest logit (log2), sum
   float2* joined; // [units, N], where the weights come from K again
   float* stash;   // [units, blocks, N, 16]
-  int chunk, n_splits;
+  int chunk, n_splits, row_waves;
 };
 AttendLayout attend_layout(const ams_params* p);
 hipError_t launch_attend(const AttendArgs& a, const AttendLayout& lay, bool bf16, int el, hipStream_t s);

@@ -178,7 +178,7 @@ int ams_attend(const ams_params* p, const ams_cache* src, const int32_t* seq_len
   a.stats = (float2*)((char*)ws + lay.stats);
   a.joined = lay.stashed ? nullptr : lay.n_splits > 1 ? (float2*)((char*)ws + lay.joined) : a.stats;
   a.stash = weights_out && lay.stashed ? (float*)((char*)ws + lay.stash) : nullptr;
-  a.chunk = lay.chunk, a.n_splits = lay.n_splits;
+  a.chunk = lay.chunk, a.n_splits = lay.n_splits, a.row_waves = lay.row_waves;
   return status(launch_attend(a, lay, p->kv_dtype == AMS_BF16, src->dtype, (hipStream_t)stream), (hipStream_t)stream);
 }
 
