@@ -69,7 +69,7 @@ class WorkspaceView(C.Structure):
 
 
 class Cache(C.Structure):
-    """A cache of any element type (cache_view).  Keeps its tensors alive; `device` is theirs."""
+    """A cache of any element type (cache_view).  Keeps its tensors alive; `index` is their GPU."""
     _fields_ = [("kv", KvView), ("dtype", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
@@ -277,7 +277,7 @@ def cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor]
         raise ValueError("int32 block table [batch, max_blocks] expected")
     kv = dense_view(k, v) if block_table is None else paged_view(k, v, block_table)
     c = Cache(kv, dtype, k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None)
-    c.tensors, c.device, c.k_dtype = tensors, k.device, k.dtype
+    c.tensors, c.index = tensors, k.get_device()
     c.lead = tuple(k.shape[:3]) if block_table is None else (k.shape[0], block_table.shape[0], k.shape[2])
     c.head_dim = k.shape[-1]
     return c
@@ -290,29 +290,32 @@ def make_rope(rot_dim: int, layout: int = ROPE_HALF, base: float = 10000.0, scal
     return r
 
 
+# The calls below run once per layer and token: their checks are written to cost the host little next to a launch (3 us).
+
 def _cache_for(p: Params, c: Cache):
+    """The GPU that the cache lies on, if it has the parameters' sizes."""
     if c.lead != (p.n_layers, p.batch, p.n_kv_heads) or c.head_dim != p.head_dim:
         raise ValueError(f"a cache of {c.lead} heads of {c.head_dim} channels does not fit the parameters")
+    return c.index
 
 
-def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, device: torch.device, what: str):
-    """Pointer of a contiguous tensor of at least `numel` elements on the call's GPU; None stays None."""
+def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, gpu: int, what: str):
+    """Pointer of a contiguous tensor of at least `numel` elements on that GPU; None stays None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.get_device() != device.index or t.numel() < numel or not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous {dtype} tensor of at least {numel} elements on {device} expected")
+    if t.dtype is not dtype or t.get_device() != gpu or t.numel() < numel or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {dtype} tensor of at least {numel} elements on GPU {gpu} expected")
     return t.data_ptr()
 
 
-def _launch(fn, what: str, device: torch.device, stream, *args):
+def _launch(fn, what: str, gpu: int, stream, *args):
     """Calls fn on the cache's GPU, whichever is current, and on that GPU's current stream unless one is given."""
-    index = device.index
     # (the raw handle of the current stream: making a Stream object of it costs as much as a launch)
-    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    if torch._C._cuda_getDevice() == index:
+    handle = torch._C._cuda_getCurrentRawStream(gpu) if stream is None else stream.cuda_stream
+    if torch._C._cuda_getDevice() == gpu:
         rc = fn(*args, handle)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(gpu):
             rc = fn(*args, handle)
     if rc != OK:
         raise AmsError(rc, what)
@@ -321,36 +324,32 @@ def _launch(fn, what: str, device: torch.device, stream, *args):
 _ROWS = {F32: torch.float32, BF16: torch.bfloat16}
 
 
-def _rows_dtype(p: Params) -> torch.dtype:
-    return _ROWS[p.kv_dtype]
-
-
-def _token_rows(t: torch.Tensor, shape, dtype, device, what: str):
+def _token_rows(t: torch.Tensor, shape, dtype, gpu: int, what: str):
     """(pointer, elements from token to token) of [L, B, n_new, heads, D]: any slice of a projection's output along the heads."""
     L, batch, n_new, heads, D = shape
-    s = t.stride()
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != device.index or s[4] != 1 or (heads > 1 and s[3] != D):
-        raise ValueError(f"{what}: {dtype} {list(shape)} (layers, batch, new, heads, channels) on {device} with contiguous heads expected")
+    s0, s1, s2, s3, s4 = t.stride() if t.dim() == 5 else (0,) * 5
+    if t.dtype is not dtype or t.get_device() != gpu or t.shape != shape or s4 != 1 or (heads > 1 and s3 != D):
+        raise ValueError(f"{what}: {dtype} {list(shape)} (layers, batch, new, heads, channels) on GPU {gpu} with contiguous heads expected")
     # one stride from token to token, over those of a sequence, the batch and the layers (extents of one have none)
-    step = s[2] if n_new > 1 else s[1] if batch > 1 else s[0] if L > 1 else heads * D
-    if (batch > 1 and s[1] != step * n_new) or (L > 1 and s[0] != step * n_new * batch):
+    step = s2 if n_new > 1 else s1 if batch > 1 else s0 if L > 1 else heads * D
+    if (batch > 1 and s1 != step * n_new) or (L > 1 and s0 != step * n_new * batch):
         raise ValueError(f"{what}: one stride from token to token expected")
     return t.data_ptr(), step
 
 
 def ams_append(p, q, k, v, q_weight, k_weight, norm_eps, rope, positions, seq_lens, q_out, dst, lens_out=None, stream=None):
     """q [L, B, n_new, H * G, D] (or None, q_out too), k, v [L, B, n_new, H, D]; rope, the weights, positions and lens_out may be None."""
-    _cache_for(p, dst)
-    L, batch, H, D, n_new = p.n_layers, p.batch, p.n_kv_heads, p.head_dim, k.shape[2]
-    dev, rows, HQ = dst.device, _ROWS[p.kv_dtype], H * p.group
-    qp, qs = _token_rows(q, (L, batch, n_new, HQ, D), rows, dev, "q") if q is not None else (None, 0)
-    kp, ks = _token_rows(k, (L, batch, n_new, H, D), rows, dev, "k")
-    vp, vs = _token_rows(v, (L, batch, n_new, H, D), rows, dev, "v")
-    x = NewTokens(qp, kp, vp, qs, ks, vs, _arg(q_weight, rows, D, dev, "q_weight"), _arg(k_weight, rows, D, dev, "k_weight"), norm_eps,
-                  _arg(positions, torch.int32, batch, dev, "positions"), n_new)
-    _launch((_lib or lib()).ams_append, "ams_append", dev, stream, C.byref(p), C.byref(x), C.byref(rope) if rope is not None else None,
-            _arg(seq_lens, torch.int32, batch, dev, "seq_lens"), _arg(q_out, rows, L * batch * HQ * n_new * D, dev, "q_out"), C.byref(dst),
-            _arg(lens_out, torch.int32, batch, dev, "lens_out"))
+    gpu = _cache_for(p, dst)
+    (L, batch, H), D, n_new, rows, i32 = dst.lead, dst.head_dim, k.shape[2], _ROWS[p.kv_dtype], torch.int32
+    HQ, kv_shape = H * p.group, (L, batch, n_new, H, D)
+    qp, qs = _token_rows(q, (L, batch, n_new, HQ, D), rows, gpu, "q") if q is not None else (None, 0)
+    kp, ks = _token_rows(k, kv_shape, rows, gpu, "k")
+    vp, vs = _token_rows(v, kv_shape, rows, gpu, "v")
+    x = NewTokens(qp, kp, vp, qs, ks, vs, _arg(q_weight, rows, D, gpu, "q_weight"), _arg(k_weight, rows, D, gpu, "k_weight"), norm_eps,
+                  _arg(positions, i32, batch, gpu, "positions"), n_new)
+    _launch((_lib or lib()).ams_append, "ams_append", gpu, stream, C.byref(p), C.byref(x), C.byref(rope) if rope is not None else None,
+            _arg(seq_lens, i32, batch, gpu, "seq_lens"), _arg(q_out, rows, L * batch * HQ * n_new * D, gpu, "q_out"), C.byref(dst),
+            _arg(lens_out, i32, batch, gpu, "lens_out"))
 
 
 def ams_attend_workspace_bytes(p: Params) -> int:
@@ -358,28 +357,25 @@ def ams_attend_workspace_bytes(p: Params) -> int:
 
 
 def ams_attend(p, src, seq_lens, q, out, ws, lse=None, weights_in=None, weights_out=None, stream=None):
-    _cache_for(p, src)
-    dev, rows = src.device, _rows_dtype(p)
+    gpu, rows = _cache_for(p, src), _ROWS[p.kv_dtype]
     n = p.units * p.group * p.window
-    _launch((_lib or lib()).ams_attend, "ams_attend", dev, stream, C.byref(p), C.byref(src),
-            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"), _arg(q, rows, n * p.head_dim, dev, "q"),
-            _arg(out, rows, n * p.head_dim, dev, "out"), _arg(lse, torch.float32, n, dev, "lse"),
-            _arg(weights_in, torch.float32, p.units * p.t_stride, dev, "weights_in"),
-            _arg(weights_out, torch.float32, p.units * p.t_stride, dev, "weights_out"),
-            _arg(ws, torch.uint8, 0, dev, "ws"), ws.numel())
+    _launch((_lib or lib()).ams_attend, "ams_attend", gpu, stream, C.byref(p), C.byref(src),
+            _arg(seq_lens, torch.int32, p.batch, gpu, "seq_lens"), _arg(q, rows, n * p.head_dim, gpu, "q"),
+            _arg(out, rows, n * p.head_dim, gpu, "out"), _arg(lse, torch.float32, n, gpu, "lse"),
+            _arg(weights_in, torch.float32, p.units * p.t_stride, gpu, "weights_in"),
+            _arg(weights_out, torch.float32, p.units * p.t_stride, gpu, "weights_out"),
+            _arg(ws, torch.uint8, 0, gpu, "ws"), ws.numel())
 
 
 def ams_recode(p, src, seq_lens, dst, idx=None, n_kept=None, credit_src=None, credit_dst=None, stream=None):
-    _cache_for(p, src)
-    _cache_for(p, dst)
-    dev = src.device
-    if dst.device != dev:
+    gpu = _cache_for(p, src)
+    if _cache_for(p, dst) != gpu:
         raise ValueError("both caches lie on one GPU")
-    _launch((_lib or lib()).ams_recode, "ams_recode", dev, stream, C.byref(p), C.byref(src),
-            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"), _arg(idx, torch.int32, p.units * p.budget, dev, "idx"),
-            _arg(n_kept, torch.int32, p.units, dev, "n_kept"), C.byref(dst),
-            _arg(credit_src, torch.float32, p.units * p.t_stride, dev, "credit_src"),
-            _arg(credit_dst, torch.float32, p.units * p.budget, dev, "credit_dst"))
+    _launch((_lib or lib()).ams_recode, "ams_recode", gpu, stream, C.byref(p), C.byref(src),
+            _arg(seq_lens, torch.int32, p.batch, gpu, "seq_lens"), _arg(idx, torch.int32, p.units * p.budget, gpu, "idx"),
+            _arg(n_kept, torch.int32, p.units, gpu, "n_kept"), C.byref(dst),
+            _arg(credit_src, torch.float32, p.units * p.t_stride, gpu, "credit_src"),
+            _arg(credit_dst, torch.float32, p.units * p.budget, gpu, "credit_dst"))
 
 
 def ams_evict_workspace_bytes(p: Params) -> int:
@@ -387,17 +383,15 @@ def ams_evict_workspace_bytes(p: Params) -> int:
 
 
 def ams_evict(p, src, seq_lens, weights, dst, weights_out, idx, n_kept, ws, lens_out=None, stream=None):
-    _cache_for(p, src)
-    _cache_for(p, dst)
-    dev = src.device
-    if dst.device != dev:
+    gpu = _cache_for(p, src)
+    if _cache_for(p, dst) != gpu:
         raise ValueError("both caches lie on one GPU")
-    _launch((_lib or lib()).ams_evict, "ams_evict", dev, stream, C.byref(p), C.byref(src),
-            _arg(seq_lens, torch.int32, p.batch, dev, "seq_lens"),
-            _arg(weights, torch.float32, p.units * p.t_stride, dev, "weights"), C.byref(dst),
-            _arg(weights_out, torch.float32, p.units * p.t_stride, dev, "weights_out"),
-            _arg(idx, torch.int32, p.units * p.budget, dev, "idx"), _arg(n_kept, torch.int32, p.units, dev, "n_kept"),
-            _arg(lens_out, torch.int32, p.batch, dev, "lens_out"), _arg(ws, torch.uint8, 0, dev, "ws"), ws.numel())
+    _launch((_lib or lib()).ams_evict, "ams_evict", gpu, stream, C.byref(p), C.byref(src),
+            _arg(seq_lens, torch.int32, p.batch, gpu, "seq_lens"),
+            _arg(weights, torch.float32, p.units * p.t_stride, gpu, "weights"), C.byref(dst),
+            _arg(weights_out, torch.float32, p.units * p.t_stride, gpu, "weights_out"),
+            _arg(idx, torch.int32, p.units * p.budget, gpu, "idx"), _arg(n_kept, torch.int32, p.units, gpu, "n_kept"),
+            _arg(lens_out, torch.int32, p.batch, gpu, "lens_out"), _arg(ws, torch.uint8, 0, gpu, "ws"), ws.numel())
 
 
 @dataclass
