@@ -336,7 +336,10 @@ int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t
  * appended costs the rows that are there at most half a step each time, of steps that at least double:
  * together less than one step of the final scale.  The readers take any finite scale.  Codes of
  * AMS_E4M3 that are no number are not written by the library; a caller's own make the sums they enter NaN.
- * A block table entry outside the pool is read as the nearest page and never written through.
+ * A block table entry outside the pool is read as the nearest page and never written through.  Blocks
+ * that a call writes belong to one (sequence, place in the table) alone.
+ * Outputs of the calls below overlap neither inputs nor one another unless it says so; calls that overlap in
+ * time (streams, graphs) need workspaces of their own.  Nothing is kept in a workspace from call to call.
  */
 typedef struct {
   ams_kv_view kv;
@@ -388,12 +391,13 @@ typedef struct {
  * ams_append - n_new tokens behind the seq_lens[b] rows of every sequence, in one pass: every query and key is normalised
  * over its head (x / sqrt(mean(x^2) + norm_eps) * weight; left out without a weight), then rotated, keys and values are
  * written to rows seq_lens[b] .. of the cache and the queries to q_out in the layout of ams_score and ams_attend.
- * The angles are formed in 64 bits and reduced there; what is written is rounded once (keys that go to 8 bits are normalised and rotated
- * in 64 bits).  Of p: the sizes, kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are
+ * The angles are formed in 64 bits and reduced there; what is written is rounded once (keys that go to 8 bits are normalised and
+ * rotated in 64 bits).  Of p: the sizes, kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are
  * not written (a full sequence takes nothing), so seq_lens[b] = t_max leaves a sequence of a padded batch out.
  * A block of an 8-bit cache that already holds rows takes the larger of its scale and that of the new rows; where it
  * grows the rows that are there are rounded again.  A block that the call begins takes nothing from its old scale.
- *   q_out    [dev] [layers, batch, kv_heads * group, n_new, head_dim] kv_dtype, all of it written; NULL when x->q is
+ *   q_out    [dev] [layers, batch, kv_heads * group, n_new, head_dim] kv_dtype, all of it written; not x->q; NULL when
+ *            x->q is
  *   lens_out [dev] [batch] min(seq_lens[b] + n_new, t_max), or NULL; not seq_lens itself
  * rope NULL or rot_dim 0: no rotation.
  */
@@ -416,7 +420,8 @@ size_t ams_evict_workspace_bytes(const ams_params* p);
  *   lse   [dev] fp32 [layers, batch, kv_heads * group, window], or NULL
  *   weights_in, weights_out  [dev] fp32 [units, t_stride]; entries 0 .. T-1 read and written, the others left as they are; weights_in
  *         NULL: zeros; weights_out NULL: no weights wanted; they may be the same array
- *   ws    [dev] scratch of at least ams_attend_workspace_bytes(p)
+ *   ws    [dev] scratch of at least ams_attend_workspace_bytes(p), 16-byte aligned: partial outputs of a long axis, and for up to
+ *         16 queries their logits, 4 bytes a query and position
  * Codes times queries are exact products, summed in fp32; probabilities enter the second product as two bf16 terms (16 bits), three with
  * fp32 queries.  Nothing depends on the order in which workgroups run.
  */
@@ -442,7 +447,7 @@ int ams_recode(const ams_params* p, const ams_cache* src, const int32_t* seq_len
  *   weights_out [dev] fp32 [units, t_stride]: those of the kept positions, then zeros up to t_max; not weights itself
  *   idx [dev] int32 [units, budget] kept positions, ascending, then -1; n_kept [dev] int32 [units]
  *   lens_out [dev] [batch] min(budget, seq_lens[b]), or NULL; not seq_lens itself
- *   ws  [dev] scratch of at least ams_evict_workspace_bytes(p)
+ *   ws  [dev] scratch of at least ams_evict_workspace_bytes(p), 16-byte aligned: for t_max from 16385 to 262144 two bits a position
  * Of p: the sizes, kv_dtype, t_max, t_stride, budget, n_sink, n_last.
  */
 int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const float* weights, const ams_cache* dst,

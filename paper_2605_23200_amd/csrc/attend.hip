@@ -4,12 +4,20 @@
 // S^T = K Q^T, so that a lane ends with 2 x 4 logits of ONE query (column lane % 16) at positions 4 (lane / 16) + 0..3 of both
 // tiles.  That is already the layout in which the second product, O^T = V^T P^T over the same 32 positions, wants P (its k index
 // runs over the positions in any order both operands share), so probabilities never leave the lane.  V is read as bytes of
-// 8 positions per lane and turned there: one v_perm per two elements, which the conversion to bf16 needs anyway.  Codes are bf16 numbers,
-// so q.k has exact products; the scales of the two blocks of 16 positions go to the logits and to the probabilities.
+// 8 positions per lane and turned there: one v_perm per two elements, which the conversion to bf16 needs anyway.  Codes are bf16
+// numbers, so q.k has exact products; the scales of the two blocks of 16 positions go to the logits and to the probabilities.
+// P goes in as two bf16 terms: one (2^-9) would be an error as large as the rounding of the output, fp16 would lose what a block of
+// small values under another of large ones contributes; the second product has room, the kernel is bound by memory.
 // Softmax: a running reference per query that is moved (and O rescaled) only when a logit exceeds it by 2^8; P and the
 // sums are then at most 2^8 per position, far inside bf16's and fp32's range.
-// No LDS until the four waves of a workgroup (which take the steps of their split in turn) join their sums, fixed order.
+// No LDS until the waves of a workgroup (which take the steps of their split in turn) join their sums, in fixed order.
 // The splits of a long axis are joined by attend_join_kernel, again in fixed order.
+// What bounds it: the bytes of K and V.  512 paged units of 4096 to 16384 positions: 313 us, 4.7 TB/s with the logits it writes (without
+// weights, 256 dense units of 16384: 5.5 TB/s); 4 units of 131072: 33 us of 28 at the rate of a copy.  It reads that fast because
+// tables and scales come through the scalar cache, a name of a page two steps before its codes (vector loads of them: 507 us), and
+// because no load is under a condition.  More than 32 queries are bound by instructions: 440 of the vector ALU and 48 products for 32
+// positions and 32 queries, 45 us for 8 units of 32768 positions and 128 queries.  (Sharing the conversions of four waves through
+// LDS: 52; the masks as a variant of the step: 44, but 128 against 120 for 64 units and 32 queries.)
 //
 // Weights: with up to 16 queries the logits go to scratch (4 N bytes a position, written and read once, against 2 D of K and V)
 // and the join turns them into probabilities; beyond that K is read a second time (attend_weights_kernel).
@@ -557,7 +565,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
 
 // Weights from K again, for more queries than the stash is for.  The queries' operands of the whole call lie in LDS; a wave takes 64
 // positions at a time, converts them once, runs 32 queries at a time over them, and has the next 64 on their way.  (One step per
-// workgroup, with the queries loaded for it, is latency: 172 us for 64 units of 32768 positions and 32 queries, @@ with several.)
+// workgroup, with the queries loaded for it, is latency: 172 us for 64 units of 32768 positions and 32 queries, 80 with several.)
 constexpr int kWeightRows = 32, kWeightBlocks = 4, kWeightStep = kWaves * kWeightBlocks * kBlockRows;
 template <bool BF16, int HD>
 constexpr int kWeightGroupBytes = kWeightRows / 16 * (HD / 32) * (BF16 ? 1 : 3) * 64 * 16;
@@ -721,7 +729,8 @@ AttendLayout attend_layout(const ams_params* p) {
   r.row_groups = div_up(tiles, r.row_tiles * r.row_waves);
   r.stashed = N <= 16;
   // Positions per workgroup: 512 where that fills the chip several times over (ragged sequences end at different times), else
-  // as many as give one round of workgroups, three on a CU.
+  // as many as give one round of workgroups, three on a CU (two with more than 16 queries).  Us a pass, 512 ragged paged units of up to
+  // 16384: 350 with 512, 356 with 1024, 390 with 2048, 437 with 4096; 4 units of 131072: 45.6 with 512, 44.7 in one round, 48 in two.
   const size_t per_split = units * r.row_groups;
   const size_t fine = per_split * div_up(p->t_max, 512);
   if (fine >= 2048) {

@@ -81,7 +81,7 @@ int status(hipError_t e, hipStream_t s) {
   return e == hipErrorNotSupported ? AMS_ERR_UNSUPPORTED : AMS_ERR_HIP;
 }
 
-// Gather of idx's rows whatever the element types (ams_evict); both of kv_dtype: the plain compaction.
+// For the plain compaction, when both caches hold rows of kv_dtype.
 KvDev plain_view(const CacheDev& c, int layout) {
   KvDev k;
   k.base = c.base, k.block_table = c.table, k.t_capacity = c.t_capacity, k.n_slots = c.n_slots;
@@ -125,7 +125,8 @@ int ams_append(const ams_params* p, const ams_new_tokens* x, const ams_rope* rop
   int rc = check_sizes(p);
   if (rc) return rc;
   if ((rc = check_cache(p, dst, p->t_max))) return rc;
-  if (!x || !x->k || !x->v || !seq_lens || (x->q == nullptr) != (q_out == nullptr) || lens_out == seq_lens) return AMS_ERR_INVALID_ARG;
+  if (!x || !x->k || !x->v || !seq_lens || (x->q == nullptr) != (q_out == nullptr) || (q_out && q_out == x->q) || lens_out == seq_lens)
+    return AMS_ERR_INVALID_ARG;
   if (x->n_new < 1 || !(x->norm_eps >= 0.f) || isinf(x->norm_eps)) return AMS_ERR_INVALID_ARG;
   if (x->n_new > (1 << 20)) return AMS_ERR_UNSUPPORTED;
   const int es = p->kv_dtype == AMS_BF16 ? 2 : 4;

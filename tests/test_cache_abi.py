@@ -44,7 +44,7 @@ def _tokens(**kw):
     return B.NewTokens(*d.values())
 
 
-def _append(p, c, x, rope=None, lens=PTR, q_out=PTR, lens_out=None):
+def _append(p, c, x, rope=None, lens=PTR, q_out=1 << 20, lens_out=None):
     return B.lib().ams_append(C.byref(p), C.byref(x), C.byref(rope) if rope is not None else None, lens, q_out, C.byref(c), lens_out, None)
 
 
@@ -104,7 +104,7 @@ def test_evict_refusals():
     p = _p()
     src, dst = _dense(), _dense(base=1 << 20)
     for kw in (dict(lens=None), dict(w=None), dict(wout=None), dict(wout=PTR), dict(idx=None), dict(n_kept=None), dict(ws=None),
-               dict(lens_out=PTR)):
+               dict(ws=PTR + 8), dict(lens_out=PTR)):
         assert _evict(p, src, dst, **kw) == B.ERR_INVALID_ARG, kw
     assert _evict(p, src, src) == B.ERR_INVALID_ARG
     assert _evict(p, src, dst, n=B.ams_evict_workspace_bytes(p) - 1) == B.ERR_WORKSPACE_TOO_SMALL
@@ -121,6 +121,7 @@ def test_append_refusals():
                dict(k_stride=511), dict(v_stride=500), dict(k_stride=516), dict(q_stride=1028)):
         assert _append(p, c, _tokens(**kw)) == B.ERR_INVALID_ARG, kw
     assert _append(p, c, _tokens(), q_out=None) == B.ERR_INVALID_ARG
+    assert _append(p, c, _tokens(q=2 * PTR), q_out=2 * PTR) == B.ERR_INVALID_ARG       # in place
     assert _append(p, c, _tokens(), lens=None) == B.ERR_INVALID_ARG
     assert _append(p, c, _tokens(), lens_out=PTR) == B.ERR_INVALID_ARG
     assert _append(p, c, _tokens(n_new=(1 << 20) + 1)) == B.ERR_UNSUPPORTED

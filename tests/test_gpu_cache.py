@@ -413,7 +413,8 @@ def _attend_case(cache, lens, group, W, dtype="bf16", causal=False, weights="new
                     x = got_lse[l, b, h * group:(h + 1) * group].reshape(-1).double().cpu().numpy()
                     empty = ~np.isfinite(want_lse)
                     assert (x[empty] == -np.inf).all()
-                    assert (np.abs(x - want_lse)[~empty] <= (err_p + 2.0 ** -22 * np.abs(want_lse))[~empty]).all()
+                    x, y, e = x[~empty], want_lse[~empty], err_p[~empty]
+                assert (np.abs(x - y) <= e + 2.0 ** -22 * np.abs(y)).all()
                 if weights:
                     x = w_out[unit].double().cpu().numpy()
                     start = w_in[unit, :T].double().numpy() if weights != "zero" else np.zeros(T)
@@ -497,6 +498,52 @@ def test_attend_small_probabilities_with_large_values():
     want, _, _, A = _attend_reference(q.double().numpy().reshape(1, 64), cache.rows("k", 0, 0, 0, 256), cache.rows("v", 0, 0, 0, 256), 1, False)
     assert want.max() > 1e4
     assert (np.abs(out.double().cpu().numpy().reshape(1, 64) - want) <= (2.0 ** -8 + 2.0 ** -15 + 64 * 2.0 ** -24 * A[:, None]) * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_scales_of_another_writer(kind):
+    """Any finite scale: attention reads it, an append keeps it where it is large enough and rounds the rows anew where it is not."""
+    lens = [100, 37]
+    cache = _filled(kind, (1, 2, 2, 128), 160, lens, True, 24)
+    rng = np.random.default_rng(9)
+    for name in ("k_scale", "v_scale"):
+        cache.t[name] *= torch.from_numpy(rng.uniform(0.3, 3, tuple(cache.t[name].shape)).astype(np.float32))
+    _attend_case(cache, lens, 3, 2, causal=True)
+    shape = (1, 1, 1, 64)
+    cache = _filled(kind, shape, 32, [5], False, 25)
+    old = cache.t["k"][0, 0, 0, :5].float().double().numpy()
+    for had, loud in ((0.75, 1.0), (0.75, 1000.0)):
+        cache.t["k_scale"][0, 0, 0, 0] = had
+        cache.t["k"][0, 0, 0, :5] = as_code_tensor(old, kind)
+        view = cache.upload()
+        row = torch.full((1, 1, 1, 1, 64), loud, dtype=torch.bfloat16, device=DEV)
+        B.ams_append(params(shape, 32), None, row, row, None, None, 0.0, None, None, lens_dev([5]), None, view)
+        new = cache.dev["k_scale"][0, 0, 0, 0].item()
+        need = 2.0 ** -6 if kind == "int8" else 2.0 ** -8
+        need = need * (1.0 if loud == 1.0 else 1024.0 if loud / 512 > (127 / 64 if kind == "int8" else 1.75) else 512.0)
+        assert new == max(had, need)
+        codes = cache.dev["k"][0, 0, 0, :6].float().double().cpu().numpy()
+        want = old if new == had else round_codes(old * (had / new), kind)
+        assert (codes[:5] == want).all()
+        assert np.abs(codes[5] * new - loud).max() <= (new / 2 if kind == "int8" else loud / 16) * (1 + 1e-6)
+
+
+def test_attend_through_a_bad_table_entry_stays_in_the_pool():
+    """An entry outside the pool is the nearest page: the same as a table that names that page."""
+    cache = _filled("int8", (1, 1, 2, 64), 64, [64], True, 26)
+    n_pages = cache.t["k"].shape[1] // BLOCK
+    p = params((1, 1, 2, 64), 64, group=2)
+    q = torch.randn((1, 1, 4, 1, 64), device=DEV).to(torch.bfloat16)
+    outs = []
+    for entry in (-7, 0, 1 << 30, n_pages - 1):
+        cache.table[0, 2] = entry
+        out, w = torch.zeros_like(q), torch.zeros((2, 64), device=DEV)
+        B.ams_attend(p, cache.upload(), lens_dev([64]), q, out, torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV), None,
+                     None, w)
+        outs.append((out, w))
+    for a, b in ((0, 1), (2, 3)):
+        same_bits(outs[a][0], outs[b][0])
+        same_bits(outs[a][1], outs[b][1])
 
 
 @pytest.mark.parametrize("W", [4, 24])
@@ -865,6 +912,67 @@ def test_a_captured_loop_replays():
         torch.cuda.synchronize()
         for a, b in zip(want, (s["out"], s["side"][0]["w"], s["side"][1]["w"], s["side"][1]["k"])):
             same_bits(a, b, f"replay {i}")
+
+
+@pytest.mark.parametrize("W,T", [(1, 20000), (24, 20000), (40, 3000)])
+def test_captured_calls_follow_the_lengths(W, T):
+    """Attention (every way to the weights), an eviction (long rows with their marks) and the way back to rows in one graph, captured before
+    any of them has run; replays with other lengths, queries and weights, other work between, each against eager calls."""
+    shape, group, budget = (1, 3, 1, 64), 4, 700
+    src = _filled("e4m3", shape, T, [T] * 3, True, 27)
+    cache = src.upload()
+    p = params(shape, T, group=group, window=W, dtype="bf16", causal=True, budget=budget, n_sink=4, n_last=32)
+    z = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device=DEV)
+    q, lens, w_in = z(1, 3, group, W, 64, dtype=torch.bfloat16), lens_dev([T] * 3), z(3, T)
+
+    def fresh():
+        packed = HostCache("int8", shape, budget, False, 28)
+        back = HostCache("bf16", shape, budget, False, 29)
+        return dict(packed=packed.upload(), p_dev=packed.dev, back=back.upload(), b_dev=back.dev, out=torch.zeros_like(q), w=z(3, T), w_out=z(3, T),
+                    lse=z(1, 3, group, W), idx=z(3, budget, dtype=torch.int32), n_kept=z(3, dtype=torch.int32), lens_out=z(3, dtype=torch.int32),
+                    ws=z(B.ams_attend_workspace_bytes(p), dtype=torch.uint8), ws2=z(B.ams_evict_workspace_bytes(p), dtype=torch.uint8))
+
+    p_back = params(shape, budget)
+
+    def calls(s):
+        B.ams_attend(p, cache, lens, q, s["out"], s["ws"], s["lse"], w_in, s["w"])
+        B.ams_evict(p, cache, lens, s["w"], s["packed"], s["w_out"], s["idx"], s["n_kept"], s["ws2"], s["lens_out"])
+        B.ams_recode(p_back, s["packed"], s["lens_out"], s["back"])
+
+    names = ("out", "w", "lse", "w_out", "idx", "n_kept", "lens_out")
+    captured = fresh()
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        calls(captured)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    for replay, n in enumerate(([T, T // 2, 5], [1, T, T - 17], [0, 16, 900], [T, T, T])):
+        lens.copy_(torch.tensor(n, dtype=torch.int32))
+        q.copy_(torch.randn(q.shape, device=DEV, generator=gen))
+        w_in.copy_(torch.rand(w_in.shape, device=DEV, generator=gen) ** 8)
+        for name in names:                              # what a call leaves alone is the same on both sides
+            captured[name].fill_(-1)
+        for k in ("p_dev", "b_dev"):
+            for t in captured[k].values():
+                t.view(torch.uint8).fill_(0)
+        eager = fresh()
+        for name in names:
+            eager[name].fill_(-1)
+        for k in ("p_dev", "b_dev"):
+            for t in eager[k].values():
+                t.view(torch.uint8).fill_(0)
+        graph.replay()
+        torch.randn(5000, device=DEV).sum().item()
+        calls(eager)
+        torch.cuda.synchronize()
+        for name in names:
+            same_bits(captured[name], eager[name], f"replay {replay}: {name}")
+        for k in ("p_dev", "b_dev"):
+            for name in captured[k]:
+                same_bits(captured[k][name], eager[k][name], f"replay {replay}: {k} {name}")
+        assert captured["lens_out"].tolist() == [min(x, budget) for x in n]
 
 
 def test_two_streams_at_once():
