@@ -414,7 +414,7 @@ def _attend_case(cache, lens, group, W, dtype="bf16", causal=False, weights="new
                     empty = ~np.isfinite(want_lse)
                     assert (x[empty] == -np.inf).all()
                     x, y, e = x[~empty], want_lse[~empty], err_p[~empty]
-                assert (np.abs(x - y) <= e + 2.0 ** -22 * np.abs(y)).all()
+                    assert (np.abs(x - y) <= e + 2.0 ** -22 * np.abs(y)).all()
                 if weights:
                     x = w_out[unit].double().cpu().numpy()
                     start = w_in[unit, :T].double().numpy() if weights != "zero" else np.zeros(T)
