@@ -450,68 +450,74 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
 
 __device__ __forceinline__ int splits_of(const AttendArgs& a, int T) { return max(1, (T + a.chunk - 1) / a.chunk); }
 
-// (largest logit, sum) of a query from its splits, for all lanes of the wave.
+// (largest logit, sum) of a query from its splits, for the LANES lanes that ask for it together; loads in batches, since a batch is a
+// latency.
+template <int LANES>
 __device__ __forceinline__ float2 joined_stats(const AttendArgs& a, int unit, int n, int n_splits, int lane) {
+  constexpr int BATCH = LANES == 64 ? 2 : 4;
   const float2* at = a.stats + ((int64_t)unit * a.d.N + n) * a.n_splits;
-  float top = kLowest;
-  for (int s = lane; s < n_splits; s += 64) top = fmaxf(top, at[s].x);
+  float top = kLowest, sum = 0.f;
+  for (int s0 = lane; s0 < n_splits; s0 += BATCH * LANES) {
+    float2 x[BATCH];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  float sum = 0.f;
-  for (int s = lane; s < n_splits; s += 64) sum = fmaf(power_of_two(at[s].x - top), at[s].y, sum);
+    for (int i = 0; i < BATCH; ++i) x[i] = at[min(s0 + i * LANES, n_splits - 1)];
+    float now = top;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  return make_float2(top, sum);
+    for (int i = 0; i < BATCH; ++i) now = fmaxf(now, x[i].x);
+    sum *= power_of_two(top - now);
+    top = now;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+      if (s0 + i * LANES < n_splits) sum = fmaf(power_of_two(x[i].x - top), x[i].y, sum);
+  }
+  float all = sixteen_max(top);
+  if constexpr (LANES == 64) all = query_max(all);
+  sum = sixteen_sum(sum * power_of_two(top - all));
+  if constexpr (LANES == 64) sum = query_sum(sum);
+  return make_float2(all, sum);
 }
 
-// Joins the splits of query n: a wave takes every fourth split, its lanes HD / 64 channels each; then the waves together.
+// Joins the splits of query n: a wave takes every fourth group of splits, HD / 4 lanes a split, four channels a lane; then the lanes
+// and waves of the same channels together.
 template <bool BF16, int HD>
 __device__ __forceinline__ void join_splits(const AttendArgs& a, int unit, int n, int splits) {
-  constexpr int PER = HD / 64;
-  __shared__ float part[kWaves][HD];
+  constexpr int LANES = HD / 4, SIDE = 64 / LANES, AHEAD = 4;
+  __shared__ __align__(16) float part[kWaves][HD];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const float2 st = joined_stats(a, unit, n, splits, lane);
   const float2* stats = a.stats + ((int64_t)unit * a.d.N + n) * a.n_splits;
-  float x[PER];
-#pragma unroll
-  for (int e = 0; e < PER; ++e) x[e] = 0.f;
-  const float* from = a.part + ((int64_t)unit * a.n_splits * a.d.N + n) * HD + lane * PER;
+  const float* from = a.part + ((int64_t)unit * a.n_splits * a.d.N + n) * HD + lane % LANES * 4;
   const int64_t step = (int64_t)a.d.N * HD;
-  for (int s0 = wave; s0 < splits; s0 += 64 * kWaves) {
-    const int mine = s0 + kWaves * lane;
-    const float f = mine < splits ? power_of_two(stats[mine].x - st.x) : 0.f;
-    const int n_here = min(64, (splits - s0 + kWaves - 1) / kWaves);
-    for (int i0 = 0; i0 < n_here; i0 += 8) {
+  const float2 st = joined_stats<64>(a, unit, n, splits, lane);
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = wave * SIDE + lane / LANES; s0 < splits; s0 += kWaves * SIDE * AHEAD) {
+    float4 y[AHEAD];
+    float f[AHEAD];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float fi = __shfl(f, i0 + i);  // 0 past the last split, which is read again
-        const float* at = from + (s0 + kWaves * min(i0 + i, n_here - 1)) * step;
+    for (int i = 0; i < AHEAD; ++i) {
+      const int s = min(s0 + i * kWaves * SIDE, splits - 1);  // (past the last split: that one again, counted 0)
+      y[i] = *(const float4*)(from + s * step);
+      f[i] = stats[s].x;
+    }
 #pragma unroll
-        for (int e = 0; e < PER; ++e) x[e] = fmaf(fi, at[e], x[e]);
-      }
+    for (int i = 0; i < AHEAD; ++i) {
+      const float w = s0 + i * kWaves * SIDE < splits ? power_of_two(f[i] - st.x) : 0.f;
+      x.x = fmaf(w, y[i].x, x.x), x.y = fmaf(w, y[i].y, x.y), x.z = fmaf(w, y[i].z, x.z), x.w = fmaf(w, y[i].w, x.w);
     }
   }
 #pragma unroll
-  for (int e = 0; e < PER; ++e) part[wave][lane * PER + e] = x[e];
+  for (int o = LANES; o < 64; o <<= 1) x.x += __shfl_xor(x.x, o), x.y += __shfl_xor(x.y, o), x.z += __shfl_xor(x.z, o), x.w += __shfl_xor(x.w, o);
+  if (lane < LANES) *(float4*)&part[wave][lane * 4] = x;
   __syncthreads();
-  if (wave > 0) return;
-  const float inverse = st.y == 0.f ? 0.f : 1.f / st.y;
-#pragma unroll
-  for (int e = 0; e < PER; ++e) {
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) x[e] += part[w][lane * PER + e];
-    x[e] *= inverse;
+  const int d = threadIdx.x;
+  if (d < HD) {
+    const float y = (part[0][d] + part[1][d] + part[2][d] + part[3][d]) * (st.y == 0.f ? 0.f : 1.f / st.y);
+    const int64_t at = ((int64_t)unit * a.d.N + n) * HD + d;
+    if constexpr (BF16)
+      *(uint16_t*)(a.out + at * 2) = (uint16_t)bf16_pair(y, 0.f);
+    else
+      *(float*)(a.out + at * 4) = y;
   }
-  const int64_t at = ((int64_t)unit * a.d.N + n) * HD + lane * PER;
-  if constexpr (!BF16) {
-#pragma unroll
-    for (int e = 0; e < PER; ++e) ((float*)a.out)[at + e] = x[e];
-  } else if constexpr (PER == 2) {
-    *(uint32_t*)(a.out + at * 2) = bf16_pair(x[0], x[1]);
-  } else {
-    *(uint16_t*)(a.out + at * 2) = (uint16_t)bf16_pair(x[0], 0.f);
-  }
-  if (lane == 0) {
+  if (threadIdx.x == 0) {
     if (a.lse) a.lse[(int64_t)unit * a.d.N + n] = st.y == 0.f ? -INFINITY : (st.x + log2f(st.y)) * kLn2;
     if (a.joined) a.joined[(int64_t)unit * a.d.N + n] = st;
   }
@@ -533,17 +539,10 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
   }
   const int first = ((int)blockIdx.x - joins) * kStashKeys;
   if (first >= T) return;
-  {  // sixteen lanes a query
-    const int n = threadIdx.x >> 4, c = threadIdx.x & 15;
-    const float2* at = a.stats + ((int64_t)unit * N + min(n, N - 1)) * a.n_splits;
-    float2 mine = make_float2(kLowest, 0.f);
-    for (int s = c; s < splits; s += 16) {
-      const float2 x = at[s];
-      const float top = fmaxf(mine.x, x.x);
-      mine = make_float2(top, mine.y * power_of_two(mine.x - top) + x.y * power_of_two(x.x - top));
-    }
-    const float top = sixteen_max(mine.x), sum = sixteen_sum(mine.y * power_of_two(mine.x - top));
-    if (c == 0) stat[n] = make_float2(top, sum == 0.f ? 0.f : 1.f / sum);
+  {
+    const int n = threadIdx.x >> 4;
+    const float2 st = joined_stats<16>(a, unit, min(n, N - 1), splits, threadIdx.x & 15);
+    if ((threadIdx.x & 15) == 0) stat[n] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
   }
   __syncthreads();
   const int t = first + 4 * threadIdx.x;
