@@ -325,48 +325,73 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
       kt[1].load(u, slot[1], off.k[1]);
       find(next + stride);
     }
-    bf16x8 p[R][PTERMS];
+    float x[R][8];
+    bool higher = false;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float x[8];
-      float top = -INFINITY;
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = s[j >> 2][r][j & 3] * kscale[j >> 2];
-      if (!whole) {
+      for (int j = 0; j < 8; ++j) x[r][j] = s[j >> 2][r][j & 3] * kscale[j >> 2];
+    if (!whole) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (at + (j >> 2) * 16 + 4 * g + (j & 3) >= limit[r]) x[j] = -INFINITY;
-      }
+          if (at + (j >> 2) * 16 + 4 * g + (j & 3) >= limit[r]) x[r][j] = -INFINITY;
+    }
+    float top[R];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
-      if (__any(top > m[r] + kSlack)) {
-        const float now = fmaxf(m[r], query_max(top)), shrink = power_of_two(m[r] - now);
+    for (int r = 0; r < R; ++r) {
+      top[r] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top[r] = fmaxf(top[r], x[r][j]);
+      higher = higher || top[r] > m[r] + kSlack;
+    }
+    if (__any(higher)) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float now = fmaxf(m[r], query_max(top[r])), shrink = power_of_two(m[r] - now);
         m[r] = now;
         sum[r] *= shrink;
 #pragma unroll
         for (int e = 0; e < TILES; ++e) o[r][e] *= shrink;
       }
-      if (R == 1 && a.stash && c < N) {
-        float* to = a.stash + (((int64_t)unit * ((a.d.t_max + 15) / 16) + at / 16) * N + c) * 16 + 4 * g;
-        *(float4*)to = make_float4(x[0], x[1], x[2], x[3]);
-        if (at + 16 < T) *(float4*)(to + N * 16) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+    if (R == 1 && a.stash && c < N) {
+      float* to = a.stash + (((int64_t)unit * ((a.d.t_max + 15) / 16) + at / 16) * N + c) * 16 + 4 * g;
+      *(float4*)to = make_float4(x[0][0], x[0][1], x[0][2], x[0][3]);
+      if (at + 16 < T) *(float4*)(to + N * 16) = make_float4(x[0][4], x[0][5], x[0][6], x[0][7]);
+    }
+    float vscale[2] = {vt.scale[0], vt.scale[1]};
+    if (vscale[0] != vscale[0] || vscale[1] != vscale[1]) {  // a block of V that is no number: the outputs of the queries that see it, no others
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (vscale[j] == vscale[j]) continue;
+        vscale[j] = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          bool seen = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) seen = seen || !(x[r][4 * j + i] == -INFINITY);
+          const float no_number = query_max(seen ? 1.f : 0.f) > 0.f ? __uint_as_float(0x7FC00000u) : 0.f;
+#pragma unroll
+          for (int e = 0; e < TILES; ++e) o[r][e] += no_number;
+        }
       }
+    }
+    // From here on nothing branches: exponentials, conversions and products can be mixed.
+    bf16x8 p[R][PTERMS];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
       uint32_t t[3][4];
 #pragma unroll
       for (int j = 0; j < 8; j += 2) {
-        float p0 = power_of_two(x[j] - m[r]), p1 = power_of_two(x[j + 1] - m[r]);
+        float p0 = power_of_two(x[r][j] - m[r]), p1 = power_of_two(x[r][j + 1] - m[r]);
         sum[r] += p0 + p1;
-        p0 *= vt.scale[j >> 2], p1 *= vt.scale[j >> 2];
-        if (!whole) {  // a scale that is no number at a position that the query does not see
-          if (x[j] == -INFINITY) p0 = 0.f;
-          if (x[j + 1] == -INFINITY) p1 = 0.f;
-        }
-        t[0][j >> 1] = bf16_pair(p0, p1);
-        p0 -= __uint_as_float(t[0][j >> 1] << 16), p1 -= __uint_as_float(t[0][j >> 1] & 0xFFFF0000u);
-        t[1][j >> 1] = bf16_pair(p0, p1);
-        if constexpr (PTERMS == 3) {
-          p0 -= __uint_as_float(t[1][j >> 1] << 16), p1 -= __uint_as_float(t[1][j >> 1] & 0xFFFF0000u);
-          t[2][j >> 1] = bf16_pair(p0, p1);
+        p0 *= vscale[j >> 2], p1 *= vscale[j >> 2];
+#pragma unroll
+        for (int k = 0; k < PTERMS; ++k) {
+          t[k][j >> 1] = bf16_pair(p0, p1);
+          if (k + 1 < PTERMS) p0 -= __uint_as_float(t[k][j >> 1] << 16), p1 -= __uint_as_float(t[k][j >> 1] & 0xFFFF0000u);
         }
       }
 #pragma unroll
