@@ -705,8 +705,9 @@ hipError_t launch_weights(AttendArgs a, hipStream_t s) {
   constexpr int kMost = 96 * 1024 / kWeightGroupBytes<BF16, HD> * kWeightRows;  // queries whose operands fit LDS (fp32, 128 channels: 128)
   for (int row = 0; row < a.d.N; row += kMost) {
     const int end = min(a.d.N, row + kMost), bytes = div_up(end - row, kWeightRows) * kWeightGroupBytes<BF16, HD>;
-    // steps per workgroup: one round of workgroups, two on a CU, where there are more
-    const int total = div_up(a.d.t_max, kWeightStep), steps = max(1, (int)((int64_t)total * a.d.units / 512));
+    // steps per workgroup: one round of workgroups where there are more, two on a CU, or one where the queries fill its LDS (us a
+    // pass, 8 units and 128 queries: 78 with 256, 72 with 512, 77 with 1024 and 2048 workgroups; fp32: 64 with 256, 72 with 512)
+    const int total = div_up(a.d.t_max, kWeightStep), steps = max(1, (int)((int64_t)total * a.d.units / (bytes > 80 * 1024 ? 256 : 512)));
     hipError_t e = ensure_lds<attend_weights_kernel<EL, BF16, HD>>(bytes);
     if (e != hipSuccess) return e;
     prof_mark("attend_weights", s);
@@ -753,14 +754,15 @@ AttendLayout attend_layout(const ams_params* p) {
   r.row_groups = div_up(tiles, r.row_tiles * r.row_waves);
   r.stashed = N <= 16;
   // Positions per workgroup: 512 where that fills the chip several times over (ragged sequences end at different times), else
-  // as many as give one round of workgroups, three on a CU (two with more than 16 queries).  Us a pass, 512 ragged paged units of up to
+  // as many as give one round of workgroups, three on a CU (two with more than 16 queries; one
+  // fewer with fp32 queries of 128 channels, whose three terms take the registers: 64 us with 256 workgroups, 74 with 512, 96 with 1024).  Us a pass, 512 ragged paged units of up to
   // 16384: 350 with 512, 356 with 1024, 390 with 2048, 437 with 4096; 4 units of 131072: 45.6 with 512, 44.7 in one round, 48 in two.
-  const size_t per_split = units * r.row_groups;
+  const size_t per_split = units * r.row_groups, resident = (r.row_tiles == 1 ? 3 : 2) - (p->kv_dtype == AMS_F32 && p->head_dim == 128);
   const size_t fine = per_split * div_up(p->t_max, 512);
   if (fine >= 2048) {
     r.chunk = 512;
   } else {
-    const int splits = (int)max((size_t)1, (size_t)(r.row_tiles == 1 ? 768 : 512) / per_split);
+    const int splits = (int)max((size_t)1, 256 * resident / per_split);
     r.chunk = div_up(div_up(p->t_max, splits), kWaves * kStep) * kWaves * kStep;
   }
   while (div_up(p->t_max, r.chunk) > 4096) r.chunk *= 2;  // what the join goes through
