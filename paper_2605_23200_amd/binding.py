@@ -340,6 +340,8 @@ def _token_rows(t: torch.Tensor, shape, dtype, gpu: int, what: str):
 def ams_append(p, q, k, v, q_weight, k_weight, norm_eps, rope, positions, seq_lens, q_out, dst, lens_out=None, stream=None):
     """q [L, B, n_new, H * G, D] (or None, q_out too), k, v [L, B, n_new, H, D]; rope, the weights, positions and lens_out may be None."""
     gpu = _cache_for(p, dst)
+    if k.dim() != 5:
+        raise ValueError("k: [layers, batch, new, heads, channels] expected")
     (L, batch, H), D, n_new, rows, i32 = dst.lead, dst.head_dim, k.shape[2], _ROWS[p.kv_dtype], torch.int32
     HQ, kv_shape = H * p.group, (L, batch, n_new, H, D)
     qp, qs = _token_rows(q, (L, batch, n_new, HQ, D), rows, gpu, "q") if q is not None else (None, 0)

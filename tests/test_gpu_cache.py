@@ -1018,7 +1018,7 @@ def test_binding_refusals():
     assert e.value.status == B.ERR_WORKSPACE_TOO_SMALL
     row = torch.zeros((1, 1, 1, 2, 64), dtype=torch.bfloat16, device=DEV)
     wide = torch.zeros((1, 1, 1, 2, 128), dtype=torch.bfloat16, device=DEV)
-    for k in (row.cpu(), row.float(), row[..., :32], wide[..., ::2], row[:, :, :, :1]):
+    for k in (row.cpu(), row.float(), row[..., :32], wide[..., ::2], row[:, :, :, :1], row[0], row[0, 0, 0, 0]):
         with pytest.raises(ValueError):
             B.ams_append(p, None, k, row, None, None, 0.0, None, None, lens, None, view)
     t = cache.dev
