@@ -9,8 +9,8 @@
 // exchange, and four cosines and sines in one LDS read each.  (Eight channels in a row, with the other halves and interleaved
 // cosines and sines out of LDS, took 35 us for 2036 tokens of 48 heads against 23: every read hit the same banks.)  Halves that are no
 // multiple of four channels find the other channel in LDS.
-// What bounds it: a launch and its chain of latencies for single tokens (5 us for one, 8 for 64 sequences); 64-bit arithmetic of the
-// keys for long pieces (20 us for 2036 tokens of 48 heads to 8 bits, of 10 that the bytes take; 26 for 4096 tokens to bf16, 2048 each).
+// What bounds it: a launch and its chain of latencies for single tokens (5 us for one, 7 for 64 sequences); 64-bit arithmetic of the
+// keys for long pieces (17 us for 2036 tokens of 48 heads to 8 bits, of 10 that the bytes take; 27 for 4096 tokens to bf16, 2048 each).
 // Angles: position * (frequency / 2 pi) in 64 bits, whole turns taken off there: at position 10^6 fp32 would be off by 0.06 rad.
 // Keys that go to 8 bits are normalised and rotated in 64 bits: a code changes by a whole step where the value
 // crosses the middle between two, and fp32 takes about one key element in a million across.
@@ -105,7 +105,7 @@ __device__ __forceinline__ void lane_runs(const Rotation& rot, int i, int& a, in
 }
 
 // Norm and rotation of the wave's rows: channels a .. a + 3 and b .. b + 3 of row x -> y.
-template <typename M, int HD>
+template <typename M, int HD, bool ANY>
 __device__ __forceinline__ void normed_and_turned(const float (&x)[8], const float (&weight)[8], bool norm, float eps, const Rotation& rot,
                                                   const M* cos_row, const M* sin_row, M* exchange, int i, M (&y)[8]) {
 #pragma unroll
@@ -118,8 +118,8 @@ __device__ __forceinline__ void normed_and_turned(const float (&x)[8], const flo
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] *= inverse * (M)weight[e];
   }
-  if (rot.mode == TURN_NONE) return;
-  if (rot.mode != TURN_ANY_HALVES) {
+  if constexpr (!ANY) {
+    if (rot.mode == TURN_NONE) return;
     M c[4], s[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -139,24 +139,24 @@ __device__ __forceinline__ void normed_and_turned(const float (&x)[8], const flo
         y[2 * e] = p * c[e] - q * s[e], y[2 * e + 1] = q * c[e] + p * s[e];
       }
     }
-    return;
-  }
-  const int half = rot.pairs;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own stretch of LDS: its last readers are done
+  } else {
+    const int half = rot.pairs;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own stretch of LDS: its last readers are done
 #pragma unroll
-  for (int e = 0; e < 8; ++e) exchange[8 * i + e] = y[e];
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
+    for (int e = 0; e < 8; ++e) exchange[8 * i + e] = y[e];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int d = 8 * i + e;
-    if (d >= 2 * half) continue;
-    const bool second = d >= half;
-    const int pair = second ? d - half : d;
-    const M c = cos_row[pair], s = sin_row[pair], other = exchange[second ? pair : d + half];
-    y[e] = second ? y[e] * c + other * s : y[e] * c - other * s;
+    for (int e = 0; e < 8; ++e) {
+      const int d = 8 * i + e;
+      if (d >= 2 * half) continue;
+      const bool second = d >= half;
+      const int pair = second ? d - half : d;
+      const M c = cos_row[pair], s = sin_row[pair], other = exchange[second ? pair : d + half];
+      y[e] = second ? y[e] * c + other * s : y[e] * c - other * s;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
-  __builtin_amdgcn_wave_barrier();
 }
 
 // Two runs of four elements of a row.
@@ -192,8 +192,9 @@ __device__ __forceinline__ void store_runs(char* row, int a, int b, const float 
   }
 }
 
-// DST: element type of the cache; BF16: of the new rows (and of a cache of kv_dtype).
-template <int DST, bool BF16, int HD>
+// DST: element type of the cache; BF16: of the new rows (and of a cache of kv_dtype); ANY: rot.mode is TURN_ANY_HALVES, and no other
+// (a kernel with both takes 180 registers and 40 KB of LDS for int8, two workgroups on a CU; without, 146 and 24 KB, three).
+template <int DST, bool BF16, int HD, bool ANY>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation rot) {
   constexpr int SRC = BF16 ? EL_BF16 : EL_F32, ES = kElBytes<SRC>;
   constexpr int LANES = HD / 8, ROWS = 64 / LANES, PASSES = kBlockRows / ROWS;
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
   using M = std::conditional_t<PACK, double, float>;  // of keys
   __shared__ Turns<float> turns;
   __shared__ Turns<M> exact;  // (unused where M is float)
-  __shared__ __align__(16) M exchange[kWaves][ROWS][HD];
+  __shared__ __align__(16) M exchange[ANY ? kWaves : 1][ANY ? ROWS : 1][ANY ? HD : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int b = blockIdx.y % a.d.B, l = blockIdx.y / a.d.B;
   const int len = seq_len(a.d, a.seq_lens, b);
@@ -213,6 +214,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
   if (count <= 0) return;
   const int H = a.d.H, HQ = a.q ? H * a.d.G : 0, n_tasks = HQ + 2 * H;
   const int i = lane % LANES, r0 = lane / LANES;
+  M* own = nullptr;
+  if constexpr (ANY) own = exchange[wave][r0];
   int run_a, run_b;
   lane_runs(rot, i, run_a, run_b);
   const int64_t token0 = ((int64_t)l * a.d.B + b) * a.n_new + (lo - len);
@@ -258,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
         if (p * ROWS >= count) break;
         const int r = p * ROWS + r0;
         float y[8];
-        normed_and_turned<float, HD>(x[p], weight, given != nullptr, a.eps, rot, turns.cos[r], turns.sin[r], (float*)exchange[wave][r0], i, y);
+        normed_and_turned<float, HD, ANY>(x[p], weight, given != nullptr, a.eps, rot, turns.cos[r], turns.sin[r], (float*)own, i, y);
         if (r < count) store_runs<SRC>(to + r * (HD * ES), run_a, run_b, y);
       }
       continue;
@@ -275,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
           cos_row = exact.cos[r], sin_row = exact.sin[r];
         else
           cos_row = turns.cos[r], sin_row = turns.sin[r];
-        normed_and_turned<M, HD>(x[p], weight, given != nullptr, a.eps, rot, cos_row, sin_row, exchange[wave][r0], i, y);
+        normed_and_turned<M, HD, ANY>(x[p], weight, given != nullptr, a.eps, rot, cos_row, sin_row, own, i, y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           if constexpr (PACK)
@@ -331,12 +334,16 @@ template <int DST, bool BF16, int HD>
 hipError_t launch(const AppendArgs& a, const Rotation& rot, hipStream_t s) {
   const int tiles = (a.n_new + 14) / kBlockRows + 1, rows = a.d.L * a.d.B;
   const int tasks = (a.q ? a.d.H * a.d.G : 0) + 2 * a.d.H;
-  // Slices of the heads: one round of workgroups, two on a CU where keys are formed in 64 bits (their registers), else four.  2036
-  // tokens of 48 heads to 8 bits: 19.9 us with 396 workgroups, 24.9 with 792, 29.8 with 1584; 4096 tokens, bf16: 39.6 with 258,
-  // 25.8 with 774, 29.4 with 1548.
-  const int slices = min(max(1, (kPacked<DST> ? 512 : 1024) / (int)min((int64_t)tiles * rows, (int64_t)1024)), div_up(tasks, kWaves));
+  // Slices of the heads: one round of workgroups, three on a CU where keys are formed in 64 bits (their registers), else four.  2036
+  // tokens of 48 heads to 8 bits: 20.0 us with 396 workgroups, 17.3 with 660, 21.9 with 924; 4096 tokens, bf16: 38.5 with 516, 25.3
+  // with 1032, 29.5 with 1548.
+  const int slices = min(max(1, (kPacked<DST> ? 768 : 1024) / (int)min((int64_t)tiles * rows, (int64_t)1024)), div_up(tasks, kWaves));
   prof_mark("append", s);
-  hipLaunchKernelGGL((append_kernel<DST, BF16, HD>), dim3(tiles, rows, slices), dim3(kThreads), 0, s, a, rot);
+  const dim3 grid(tiles, rows, slices);
+  if (rot.mode == TURN_ANY_HALVES)
+    hipLaunchKernelGGL((append_kernel<DST, BF16, HD, true>), grid, dim3(kThreads), 0, s, a, rot);
+  else
+    hipLaunchKernelGGL((append_kernel<DST, BF16, HD, false>), grid, dim3(kThreads), 0, s, a, rot);
   return hipGetLastError();
 }
 
