@@ -576,10 +576,14 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
   float w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int n = 0; n < N; ++n) {
-    const float4 s = *(const float4*)(x + n * 16);
+    const float4 v = *(const float4*)(x + n * 16);
+    const float s[4] = {v.x, v.y, v.z, v.w};
     const float2 st = stat[n];
-    w[0] = fmaf(power_of_two(s.x - st.x), st.y, w[0]), w[1] = fmaf(power_of_two(s.y - st.x), st.y, w[1]);
-    w[2] = fmaf(power_of_two(s.z - st.x), st.y, w[2]), w[3] = fmaf(power_of_two(s.w - st.x), st.y, w[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // (a position that the query does not see has no part in a sum that is no number)
+      const float p = power_of_two(s[i] - st.x) * st.y;
+      w[i] += s[i] == -INFINITY ? 0.f : p;
+    }
   }
   const int64_t at = (int64_t)unit * a.d.t_stride + t;
 #pragma unroll

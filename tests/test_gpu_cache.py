@@ -573,6 +573,25 @@ def test_attend_nan_blocks(W):
     assert torch.isnan(w[0, first * BLOCK:T]).all()
 
 
+@pytest.mark.parametrize("W", [4, 24])
+def test_attend_a_query_that_is_no_number(W):
+    """The first query of the window NaN: its output, its lse, and the weights of what it sees; not those of the positions behind it."""
+    T = 160
+    cache = _filled("e4m3", (1, 1, 1, 64), 200, [T], False, 4)
+    p = params((1, 1, 1, 64), 200, group=2, window=W, causal=True)
+    q = torch.randn((1, 1, 2, W, 64)).to(torch.bfloat16)
+    q[0, 0, 1, 0] = math.nan
+    out, lse = torch.zeros_like(q, device=DEV), torch.zeros((1, 1, 2, W), device=DEV)
+    w = torch.zeros((1, 200), device=DEV)
+    ws = torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+    B.ams_attend(p, cache.upload(), lens_dev([T]), q.to(DEV), out, ws, lse, None, w)
+    bad = torch.zeros((2, W), dtype=torch.bool)
+    bad[1, 0] = True
+    assert torch.equal(torch.isnan(out.float()).all(-1).cpu()[0, 0], bad) and torch.equal(torch.isnan(out.float()).any(-1).cpu()[0, 0], bad)
+    assert torch.equal(torch.isnan(lse).cpu()[0, 0], bad)
+    assert torch.equal(torch.isnan(w[0, :T]).cpu(), torch.arange(T) < T - W + 1)
+
+
 def test_attend_two_calls_give_the_same_bits():
     cache = _filled("e4m3", (2, 2, 4, 128), 3000, [3000, 1234], True, 11)
     for W in (1, 20):
