@@ -81,14 +81,6 @@ int status(hipError_t e, hipStream_t s) {
   return e == hipErrorNotSupported ? AMS_ERR_UNSUPPORTED : AMS_ERR_HIP;
 }
 
-// For the plain compaction, when both caches hold rows of kv_dtype.
-KvDev plain_view(const CacheDev& c, int layout) {
-  KvDev k;
-  k.base = c.base, k.block_table = c.table, k.t_capacity = c.t_capacity, k.n_slots = c.n_slots;
-  k.layout = layout, k.max_blocks = c.max_blocks, k.B = c.B, k.H = c.H, k.row_bytes = c.row_bytes;
-  return k;
-}
-
 }  // namespace
 }  // namespace ams
 
@@ -211,17 +203,11 @@ int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens
   const Dims d = dims(p);
   const EvictArgs e{d, seq_lens, weights, weights_out, idx, n_kept, lens_out, p->budget, p->n_sink, p->n_last};
   hipStream_t s = (hipStream_t)stream;
-  hipError_t err = launch_evict_pick(e, (char*)ws, s);
+  const hipError_t err = launch_evict_pick(e, (char*)ws, s);
   if (err != hipSuccess) return status(err, s);
   const CacheDev ks = device(p, src, false), vs = device(p, src, true), kd = device(p, dst, false), vd = device(p, dst, true);
-  if (!packed(src) && !packed(dst)) {
-    err = launch_compact(p, d, plain_view(ks, src->kv.layout), plain_view(vs, src->kv.layout), plain_view(kd, dst->kv.layout),
-                         plain_view(vd, dst->kv.layout), idx, n_kept, nullptr, nullptr, s);
-  } else {
-    const RecodeArgs a{d, ks, vs, kd, vd, nullptr, idx, n_kept, p->budget, nullptr, nullptr, p->budget};
-    err = launch_recode(a, src->dtype, dst->dtype, s);
-  }
-  return status(err, s);
+  const RecodeArgs a{d, ks, vs, kd, vd, nullptr, idx, n_kept, p->budget, nullptr, nullptr, p->budget};
+  return status(launch_recode(a, src->dtype, dst->dtype, s), s);
 }
 
 }  // extern "C"

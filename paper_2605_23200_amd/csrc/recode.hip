@@ -1,11 +1,13 @@
-// Gather of cache rows between element types (ams_recode): rows of kv_dtype to 8 bits, 8 bits to rows, 8 bits to 8 bits.
+// Gather of cache rows between element types (ams_recode, ams_evict): rows of kv_dtype to 8 bits, 8 bits to rows, 8 bits to 8 bits, and
+// (ams_evict) rows of kv_dtype as they are.
 // value = code * scale of its block of 16 positions; a destination block takes the scale of the largest magnitude of ITS 16
 // rows, so a block is the unit of work: one wave holds all of it in registers (eight elements per lane and row: 16 lanes a
 // row of 128 channels, four rows a load), reduces the largest magnitude over its lanes and writes codes and scale.  Every byte
 // moves once; no LDS, no barrier.  Memory is the bound: what a gathered row waits for (index, page, then scale and row) is a
 // chain of latencies, so a wave starts all rows of K and V of its block before it looks at the first: 256 units, 2048 of
 // 2176 rows, 8 bits to 8 bits: 94 us with a wave for K and one for V that loaded row by row, 52 so (5.2 TB/s); 2048 of 32768 bf16 rows
-// to 8 bits: 96 and 83 (4.9 TB/s); 96 paged units, rows of 128 bytes scattered over a pool: 51 (4.1 TB/s).
+// to 8 bits: 96 and 83 (4.9 TB/s); 96 paged units, rows of 128 bytes scattered over a pool: 51 (4.1 TB/s)  Rows of kv_dtype as they
+// are: an eviction of 256 units to 2048 of 32768 takes 162 us, with a copy that went row by row 164.
 #include "cache.h"
 
 namespace ams {
@@ -29,6 +31,12 @@ struct Raw {
         w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
       }
     }
+  }
+  __device__ __forceinline__ void store(char* at, bool real) const {  // zeros where it is not
+    static_assert(!kPacked<EL>, "rows of kv_dtype");
+#pragma unroll
+    for (int i = 0; i < (EL == EL_F32 ? 8 : 4); i += 4)
+      *(uint4*)(at + 4 * i) = real ? make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]) : make_uint4(0u, 0u, 0u, 0u);
   }
   __device__ __forceinline__ void values(float (&x)[8]) const {
     if constexpr (EL == EL_F32) {
@@ -89,6 +97,15 @@ __global__ __launch_bounds__(kThreads) void recode_kernel(RecodeArgs a) {
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
     const CacheDev& dst = kv ? a.vd : a.kd;
+    char* rows = dst.base + (to.row0 - a.kd.base) + i * 8 * kElBytes<DST>;
+    if constexpr (SRC == DST && !kPacked<DST>) {  // as they are
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        const int r = p * ROWS + r0;
+        if (blk * kBlockRows + r < n) raw[kv][p].store(rows + r * to.stride, real[p]);
+      }
+      continue;
+    }
     float x[PASSES][8];
     uint32_t top = 0;
 #pragma unroll
@@ -107,7 +124,6 @@ __global__ __launch_bounds__(kThreads) void recode_kernel(RecodeArgs a) {
       inverse = scale_inverse(s);
       if (lane == 0) dst.scale[to.scale] = s;
     }
-    char* rows = dst.base + (to.row0 - a.kd.base) + i * 8 * kElBytes<DST>;
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       const int r = p * ROWS + r0;
@@ -138,10 +154,10 @@ hipError_t launch_to(const RecodeArgs& a, int dst_el, hipStream_t s) {
     case EL_INT8: return launch<SRC, EL_INT8>(a, s);
     case EL_E4M3: return launch<SRC, EL_E4M3>(a, s);
     case EL_BF16:
-      if constexpr (kPacked<SRC>) return launch<SRC, EL_BF16>(a, s);
+      if constexpr (kPacked<SRC> || SRC == EL_BF16) return launch<SRC, EL_BF16>(a, s);
       break;
     case EL_F32:
-      if constexpr (kPacked<SRC>) return launch<SRC, EL_F32>(a, s);
+      if constexpr (kPacked<SRC> || SRC == EL_F32) return launch<SRC, EL_F32>(a, s);
       break;
   }
   return hipErrorNotSupported;

@@ -169,6 +169,29 @@ def test_a_bad_table_entry_is_never_written_through():
         dst.table[:] = good
 
 
+@pytest.mark.parametrize("src_kind,dst_kind,dtype", [("bf16", "bf16", "bf16"), ("f32", "f32", "f32"), ("int8", "bf16", "bf16"), ("bf16", "e4m3", "bf16")])
+def test_evict_never_writes_through_a_bad_table_entry(src_kind, dst_kind, dtype):
+    """The pages that the destination's table names take their rows; all others, the first and the last of the pool too, stay as they are."""
+    shape = (1, 1, 2, 64)
+    src, dst = _filled(src_kind, shape, 48, [48], True, 1), HostCache(dst_kind, shape, 48, True, 2)
+    p = params(shape, 48, dtype=dtype, budget=40)
+    w = torch.rand((2, 48), device=DEV)
+    for bad in (-1, 1 << 30):
+        good = dst.table.copy()
+        dst.table[0, 1] = bad
+        view = dst.upload()
+        had = {k: v.clone() for k, v in dst.dev.items()}
+        idx, n_kept = torch.zeros((2, 40), dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+        ws = torch.zeros(B.ams_evict_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+        B.ams_evict(p, src.upload(), lens_dev([48]), w, view, torch.empty_like(w), idx, n_kept, ws)
+        mine = (np.delete(good[0], 1)[:, None] * BLOCK + np.arange(BLOCK)).reshape(-1)
+        others = [r for r in range(dst.t["k"].shape[1]) if r not in set(mine.tolist())]
+        for name in ("k", "v"):
+            same_bits(dst.dev[name][:, others], had[name][:, others])
+            assert not torch.equal(dst.dev[name][:, mine].view(torch.uint8), had[name][:, mine].view(torch.uint8))
+        dst.table[:] = good
+
+
 # ---- ams_append -------------------------------------------------------------------------------------------------
 
 def _turned(x, weight, eps, pos, rope_kw, freq):
