@@ -395,7 +395,8 @@ typedef struct {
  * rotated in 64 bits).  Of p: the sizes, kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are
  * not written (a full sequence takes nothing), so seq_lens[b] = t_max leaves a sequence of a padded batch out.
  * A block of an 8-bit cache that already holds rows takes the larger of its scale and that of the new rows; where it
- * grows the rows that are there are rounded again.  A block that the call begins takes nothing from its old scale.
+ * grows the rows that are there are rounded again (theirs are codes that are numbers and a scale that is not negative).  A block that
+ * the call begins takes nothing from its old scale.
  *   q_out    [dev] [layers, batch, kv_heads * group, n_new, head_dim] kv_dtype, all of it written; not x->q; NULL when
  *            x->q is
  *   lens_out [dev] [batch] min(seq_lens[b] + n_new, t_max), or NULL; not seq_lens itself
@@ -423,7 +424,8 @@ size_t ams_evict_workspace_bytes(const ams_params* p);
  *   ws    [dev] scratch of at least ams_attend_workspace_bytes(p), 16-byte aligned: partial outputs of a long axis, and for up to
  *         16 queries their logits, 4 bytes a query and position
  * Codes times queries are exact products, summed in fp32; probabilities enter the second product as two bf16 terms (16 bits), three with
- * fp32 queries.  Nothing depends on the order in which workgroups run.
+ * fp32 queries.  Nothing depends on the order in which workgroups run.  Sums are divided when they are whole: values below 2^90 in
+ * magnitude (larger ones can make an output infinite or no number).
  */
 int ams_attend(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const void* q, void* out, float* lse,
                const float* weights_in, float* weights_out, void* ws, size_t ws_bytes, void* stream);
@@ -448,7 +450,7 @@ int ams_recode(const ams_params* p, const ams_cache* src, const int32_t* seq_len
  *   idx [dev] int32 [units, budget] kept positions, ascending, then -1; n_kept [dev] int32 [units]
  *   lens_out [dev] [batch] min(budget, seq_lens[b]), or NULL; not seq_lens itself
  *   ws  [dev] scratch of at least ams_evict_workspace_bytes(p), 16-byte aligned: for t_max from 16385 to 262144 two bits a position
- * Of p: the sizes, kv_dtype, t_max, t_stride, budget, n_sink, n_last.
+ * Of p: the sizes, kv_dtype, t_max, t_stride, budget (at most 2^30: AMS_ERR_UNSUPPORTED), n_sink, n_last.
  */
 int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const float* weights, const ams_cache* dst,
               float* weights_out, int32_t* idx, int32_t* n_kept, int32_t* lens_out, void* ws, size_t ws_bytes, void* stream);

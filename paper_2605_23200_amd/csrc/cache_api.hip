@@ -32,7 +32,8 @@ int check_attend(const ams_params* p) {
 int check_evict(const ams_params* p) {
   const int rc = check_sizes(p);
   if (rc) return rc;
-  return p->budget < 1 || p->n_sink < 0 || p->n_last < 0 ? AMS_ERR_INVALID_ARG : AMS_OK;
+  if (p->budget < 1 || p->n_sink < 0 || p->n_last < 0) return AMS_ERR_INVALID_ARG;
+  return p->budget > (1 << 30) ? AMS_ERR_UNSUPPORTED : AMS_OK;
 }
 
 bool packed(const ams_cache* c) { return c->dtype == AMS_INT8 || c->dtype == AMS_E4M3; }

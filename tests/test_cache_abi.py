@@ -114,6 +114,15 @@ def test_evict_refusals():
         assert _evict(q, src, dst) == B.ERR_INVALID_ARG and B.ams_evict_workspace_bytes(q) == 0
 
 
+def test_evict_budget_beyond_its_counters():
+    """The tail of a row of idx is written by a 32-bit counter in steps of a workgroup: a budget near 2^31 would carry it past its end."""
+    p = _p()
+    p.budget = (1 << 30) + 1
+    assert _evict(p, _dense(), _dense(base=1 << 20)) == B.ERR_UNSUPPORTED and B.ams_evict_workspace_bytes(p) == 0
+    p.budget = 1 << 30
+    assert B.ams_evict_workspace_bytes(p) > 0
+
+
 def test_append_refusals():
     p, c = _p(), _dense()
     for kw in (dict(k=None), dict(v=None), dict(q=None), dict(n_new=0), dict(norm_eps=-1.0), dict(norm_eps=math.inf), dict(norm_eps=math.nan),
