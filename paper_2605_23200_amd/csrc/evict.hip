@@ -8,7 +8,7 @@
 //    the equal ones stay.
 // Longer rows have two launches before that, since one compute unit reads its row at no more than 15 to 25 GB/s (96 rows of 40000 to
 // 131072 positions of which 4096 stay: 316 us with digits of the whole row from one workgroup, 112 with a sample and one
-// walk, 56 now): a sample of the row says between which two values the wanted one lies, then many workgroups mark what is above
+// walk, 53 now): a sample of the row says between which two values the wanted one lies, then many workgroups mark what is above
 // and what is between.  The digits are those of what is between.  The sample is wrong once in some thousand rows; the counts
 // show it, and the digits of the whole row decide.
 #include "cache.h"
@@ -158,19 +158,13 @@ __global__ __launch_bounds__(kThreads) void evict_bounds_kernel(EvictArgs a, Mar
 constexpr int kMarkThreads = 256, kMarkGroups = 16;                   // groups of 64 positions per wave
 constexpr int kMarkPositions = kMarkThreads / 64 * kMarkGroups * 64;  // per workgroup
 
-// The bits of the row, and the zeros behind the kept weights.
+// The bits of the row.
 __global__ __launch_bounds__(kMarkThreads) void evict_mark_kernel(EvictArgs a, Marks m) {
   const int unit = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const Rule r(a, b);
   const int t0 = blockIdx.x * kMarkPositions + wave * kMarkGroups * 64;
-  float* out = a.weights_out + (int64_t)unit * a.d.t_stride;
-#pragma unroll
-  for (int g = 0; g < kMarkGroups; ++g) {
-    const int t = t0 + g * 64 + lane;
-    if (t >= r.kept && t < a.d.t_max) out[t] = 0.f;
-  }
   if (!r.marked() || t0 >= r.T) return;
   const float* w = a.weights + (int64_t)unit * a.d.t_stride;
   const float2 bound = m.bounds[unit];
@@ -192,10 +186,26 @@ __global__ __launch_bounds__(kMarkThreads) void evict_mark_kernel(EvictArgs a, M
   }
 }
 
+// Zeros behind the kept weights of long rows, by workgroups of their own beside those that pick (they are memory, the others
+// latency: 96 rows of up to 131072 positions 105 us an eviction; zeros beside the marks 109, beside the sample 109).
+constexpr int kZeros = 64 * kThreads;  // positions per workgroup
+__device__ __forceinline__ void write_zeros(const EvictArgs& a, int group) {
+  const int groups = (a.d.t_max + kZeros - 1) / kZeros, unit = group / groups;
+  int l, b, h;
+  unit_coords(a.d, unit, l, b, h);
+  const Rule r(a, b);
+  float* out = a.weights_out + (int64_t)unit * a.d.t_stride;
+  const int begin = group % groups * kZeros, end = min(a.d.t_max, begin + kZeros);
+  for (int t = max(begin, r.kept) + threadIdx.x; t < end; t += kThreads) out[t] = 0.f;
+}
+
 // PER: positions per thread whose weights stay in registers; 0: any length, from memory.
 template <int PER>
 __global__ __launch_bounds__(kThreads) void evict_pick_kernel(EvictArgs a, Marks m) {
   __shared__ PickLds<PER> s;
+  if constexpr (PER == 0) {
+    if ((int)blockIdx.x >= a.d.units) return write_zeros(a, (int)blockIdx.x - a.d.units);
+  }
   const int unit = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
@@ -437,7 +447,7 @@ __global__ __launch_bounds__(kThreads) void evict_pick_kernel(EvictArgs a, Marks
     __syncthreads();  // before the next round's bits
   }
   for (int j = kept + (int)threadIdx.x; j < a.budget; j += kThreads) idx[j] = -1;
-  if (!m.bounds)  // else they are there
+  if constexpr (PER > 0)  // else write_zeros
     for (int j = kept + (int)threadIdx.x; j < a.d.t_max; j += kThreads) out[j] = 0.f;
   if (threadIdx.x == 0) {
     a.n_kept[unit] = kept;
@@ -470,7 +480,7 @@ hipError_t launch_evict_pick(const EvictArgs& a, char* ws, hipStream_t s) {
   else if (a.d.t_max <= 16 * kThreads)
     hipLaunchKernelGGL((evict_pick_kernel<16>), dim3(a.d.units), dim3(kThreads), 0, s, a, m);
   else
-    hipLaunchKernelGGL((evict_pick_kernel<0>), dim3(a.d.units), dim3(kThreads), 0, s, a, m);
+    hipLaunchKernelGGL((evict_pick_kernel<0>), dim3(a.d.units * (1 + div_up(a.d.t_max, kZeros))), dim3(kThreads), 0, s, a, m);
   return hipGetLastError();
 }
 
