@@ -591,16 +591,22 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
     if (t + i < T) a.weights_out[at + i] = (a.weights_in ? a.weights_in[at + i] : 0.f) + w[i];
 }
 
-// Weights from K again, for more queries than the stash is for.  The queries' operands of the whole call lie in LDS; a wave takes 64
-// positions at a time, converts them once, runs 32 queries at a time over them, and has the next 64 on their way.  (One step per
+// Weights from K again, for more queries than the stash is for.  The queries' operands of the whole call lie in LDS; a wave takes two
+// blocks of positions at a time, converts them once, runs 32 queries at a time over them, and has the next two on their way.  (One step per
 // workgroup, with the queries loaded for it, is latency: 172 us for 64 units of 32768 positions and 32 queries, 80 with several.)
-constexpr int kWeightRows = 32, kWeightBlocks = 4, kWeightStep = kWaves * kWeightBlocks * kBlockRows;
+// With fp32 queries four blocks, so that their three terms come out of LDS half as often (a pass of 8 units of 16384 and 128 queries
+// 64 us, 69 with two blocks; bf16, 64 units of 32768 and 32 queries 214 with four blocks at two workgroups on a CU, 201 with two at four).
+constexpr int kWeightRows = 32;
+template <bool BF16>
+constexpr int kWeightBlocks = BF16 ? 2 : 4;
+template <bool BF16>
+constexpr int kWeightStep = kWaves * kWeightBlocks<BF16> * kBlockRows;
 template <bool BF16, int HD>
 constexpr int kWeightGroupBytes = kWeightRows / 16 * (HD / 32) * (BF16 ? 1 : 3) * 64 * 16;
 
 template <int EL, bool BF16, int HD>
 __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, int row_begin, int row_end, int steps) {
-  constexpr int R = kWeightRows / 16, STEPS = HD / 32, TERMS = BF16 ? 1 : 3, BLOCKS = kWeightBlocks;
+  constexpr int R = kWeightRows / 16, STEPS = HD / 32, TERMS = BF16 ? 1 : 3, BLOCKS = kWeightBlocks<BF16>, STEP = kWeightStep<BF16>;
   typedef bf16x8 Group[R][STEPS][TERMS][64];
   extern __shared__ __align__(16) char lds[];
   Group* q = (Group*)lds;
@@ -611,7 +617,7 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, 
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b);
-  const int start = blockIdx.x * steps * kWeightStep;
+  const int start = blockIdx.x * steps * STEP;
   if (start >= T) return;
   const int groups = (row_end - row_begin + kWeightRows - 1) / kWeightRows, last_blk = (T - 1) / kBlockRows;
   const UnitBlocks u(a.k, a.v, l, b, h);
@@ -641,7 +647,7 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, 
   __syncthreads();
   const float to_log2 = kLog2E / sqrtf((float)HD);
   const int fewest = a.causal ? T - a.d.W + 1 : T;  // positions that every query sees
-  for (int step = 0; step < steps && first < T; ++step, first += kWeightStep) {
+  for (int step = 0; step < steps && first < T; ++step, first += STEP) {
     bf16x8 x[BLOCKS][STEPS];
     float scale[BLOCKS], w[BLOCKS][4];
 #pragma unroll
@@ -651,7 +657,7 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, 
       scale[j] = k[j].scale * to_log2;
       w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0.f;
     }
-    fetch(first + kWeightStep);
+    fetch(first + STEP);
     const bool whole = first + BLOCKS * kBlockRows <= fewest;
     for (int group = 0; group < groups; ++group) {
       floatx4 s[BLOCKS][R];
@@ -709,9 +715,11 @@ hipError_t launch_weights(AttendArgs a, hipStream_t s) {
   constexpr int kMost = 96 * 1024 / kWeightGroupBytes<BF16, HD> * kWeightRows;  // queries whose operands fit LDS (fp32, 128 channels: 128)
   for (int row = 0; row < a.d.N; row += kMost) {
     const int end = min(a.d.N, row + kMost), bytes = div_up(end - row, kWeightRows) * kWeightGroupBytes<BF16, HD>;
-    // steps per workgroup: one round of workgroups where there are more, two on a CU, or one where the queries fill its LDS (us a
-    // pass, 8 units and 128 queries: 78 with 256, 72 with 512, 77 with 1024 and 2048 workgroups; fp32: 64 with 256, 72 with 512)
-    const int total = div_up(a.d.t_max, kWeightStep), steps = max(1, (int)((int64_t)total * a.d.units / (bytes > 80 * 1024 ? 256 : 512)));
+    // Steps per workgroup: one round of workgroups where there are more, as many on a CU as its registers and LDS hold (us a pass, 8
+    // units of 32768 and 128 queries, 32 KB: 79 with 256 workgroups, 70 with 512, 69 with 1024, 74 with 2048; 256 queries, 64 KB: 69, 64
+    // and 71; fp32, 128 queries, 96 KB: 64 with 256, 71 with 512).
+    const int resident = min(BF16 ? 4 : 2, 160 * 1024 / (bytes + (int)(256 * sizeof(float2))));
+    const int total = div_up(a.d.t_max, kWeightStep<BF16>), steps = max(1, (int)((int64_t)total * a.d.units / (256 * resident)));
     hipError_t e = ensure_lds<attend_weights_kernel<EL, BF16, HD>>(bytes);
     if (e != hipSuccess) return e;
     prof_mark("attend_weights", s);
