@@ -12,11 +12,11 @@
 // sums are then at most 2^8 per position, far inside bf16's and fp32's range.
 // No LDS until the waves of a workgroup (which take the steps of their split in turn) join their sums, in fixed order.
 // The splits of a long axis are joined by attend_join_kernel, again in fixed order.
-// What bounds it: the bytes of K and V.  512 paged units of 4096 to 16384 positions: 313 us, 4.7 TB/s with the logits it writes (without
+// What bounds it: the bytes of K and V.  512 paged units of 4096 to 16384 positions: 288 us, 5.1 TB/s with the logits it writes (without
 // weights, 256 dense units of 16384: 5.5 TB/s); 4 units of 131072: 33 us of 28 at the rate of a copy.  It reads that fast because
 // tables and scales come through the scalar cache, a name of a page two steps before its codes (vector loads of them: 507 us), and
 // because no load is under a condition.  More than 32 queries are bound by instructions: 440 of the vector ALU and 48 products for 32
-// positions and 32 queries, 45 us for 8 units of 32768 positions and 128 queries.  (Sharing the conversions of four waves through
+// positions and 32 queries, 44 us for 8 units of 32768 positions and 128 queries.  (Sharing the conversions of four waves through
 // LDS: 52; the masks as a variant of the step: 44, but 128 against 120 for 64 units and 32 queries.)
 //
 // Weights: with up to 16 queries the logits go to scratch (4 N bytes a position, written and read once, against 2 D of K and V)
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
   constexpr int LD = HD + 4;  // row of the join in LDS
   __shared__ __align__(16) float joint[kWaves][16][LD];
   __shared__ float2 stat[kWaves][16];
-  const int unit = blockIdx.y, split = blockIdx.x;
+  const int unit = blockIdx.y, split = turned_x();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int g = lane >> 4, c = lane & 15;
   const int row_waves = a.row_waves, key_waves = kWaves / row_waves, stride = key_waves * kStep;
@@ -558,11 +558,11 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b), splits = splits_of(a, T);
-  if ((int)blockIdx.x < joins) {
+  if ((int)blockIdx.x < joins) {  // (first: they take longest)
     join_splits<BF16, HD>(a, unit, blockIdx.x, splits);
     return;
   }
-  const int first = ((int)blockIdx.x - joins) * kStashKeys;
+  const int first = turned_x(joins) * kStashKeys;
   if (first >= T) return;
   {
     const int n = threadIdx.x >> 4;
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, 
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b);
-  const int start = blockIdx.x * steps * STEP;
+  const int start = turned_x() * steps * STEP;
   if (start >= T) return;
   const int groups = (row_end - row_begin + kWeightRows - 1) / kWeightRows, last_blk = (T - 1) / kBlockRows;
   const UnitBlocks u(a.k, a.v, l, b, h);
@@ -765,14 +765,17 @@ AttendLayout attend_layout(const ams_params* p) {
   r.row_waves = tiles <= 2 ? 1 : tiles <= 4 ? 2 : 4;
   r.row_groups = div_up(tiles, r.row_tiles * r.row_waves);
   r.stashed = N <= 16;
-  // Positions per workgroup: 512 where that fills the chip several times over (ragged sequences end at different times), else
-  // as many as give one round of workgroups, three on a CU (two with more than 16 queries; one
-  // fewer with fp32 queries of 128 channels, whose three terms take the registers: 64 us with 256 workgroups, 74 with 512, 96 with 1024).  Us a pass, 512 ragged paged units of up to
-  // 16384: 350 with 512, 356 with 1024, 390 with 2048, 437 with 4096; 4 units of 131072: 45.6 with 512, 44.7 in one round, 48 in two.
+  // Positions per workgroup: 512 where that fills the chip several times over (ragged sequences end at different times), 2048 with more
+  // than 16 queries, whose partial outputs are no longer small beside the cache (4 N / chunk of its bytes, written and read again); else
+  // as many as give one round of workgroups, three on a CU (two with more than 16 queries; one fewer with fp32 queries of 128
+  // channels, whose three terms take the registers: 64 us with 256 workgroups, 74 with 512, 96 with 1024).  Us a pass, 512 ragged
+  // paged units of up to 16384: 324 with 512, 329 with 1024, 349 with 2048, 412 with 4096; 4 units of 131072: 45.6 with 512, 44.7 in
+  // one round, 48 in two; 256 ragged units of up to 16384 and 32 queries: 301, 281, 277, 282; 320 and 128 queries: 840, 730, 724, 781;
+  // 64 units of 32768 and 32 queries: 201, 187, 178, 172 (the last is one round).
   const size_t per_split = units * r.row_groups, resident = (r.row_tiles == 1 ? 3 : 2) - (p->kv_dtype == AMS_F32 && p->head_dim == 128);
-  const size_t fine = per_split * div_up(p->t_max, 512);
-  if (fine >= 2048) {
-    r.chunk = 512;
+  const int fine = r.row_tiles == 1 ? 512 : 2048;
+  if (per_split * div_up(p->t_max, fine) >= 2048) {
+    r.chunk = fine;
   } else {
     const int splits = (int)max((size_t)1, 256 * resident / per_split);
     r.chunk = div_up(div_up(p->t_max, splits), kWaves * kStep) * kWaves * kStep;

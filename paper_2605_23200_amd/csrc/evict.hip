@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kMarkThreads) void evict_mark_kernel(EvictArgs a, M
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const Rule r(a, b);
-  const int t0 = blockIdx.x * kMarkPositions + wave * kMarkGroups * 64;
+  const int t0 = turned_x() * kMarkPositions + wave * kMarkGroups * 64;
   if (!r.marked() || t0 >= r.T) return;
   const float* w = a.weights + (int64_t)unit * a.d.t_stride;
   const float2 bound = m.bounds[unit];
