@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int b = blockIdx.y % a.d.B, l = blockIdx.y / a.d.B;
   const int len = seq_len(a.d, a.seq_lens, b);
-  const int blk = len / kBlockRows + (int)blockIdx.x;
+  const int blk = len / kBlockRows + turned_x();
   const int lo = max(len, blk * kBlockRows), hi = min(len + a.n_new, (blk + 1) * kBlockRows);
   if (blockIdx.x == 0 && blockIdx.z == 0 && l == 0 && threadIdx.x == 0 && a.lens_out)
     a.lens_out[b] = min(len + a.n_new, a.d.t_max);

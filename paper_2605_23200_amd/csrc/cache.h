@@ -58,7 +58,8 @@ __device__ __forceinline__ Block block_at(const CacheDev& c, int l, int b, int h
 
 // blockIdx.x, from `first` on, of a (stretch of positions, unit) grid, turned from unit to unit.  Workgroups go to the eight dies in turn: where gridDim.x
 // and eight share a factor, the last stretches of all units, which short sequences of a batch leave empty, would fall to the same
-// dies.  (ams_attend, 512 units of 4096 to 16384 positions: 348 us without, 321 so; 320 of 1000 to 16384, 128 queries: 884 and 620.)
+// dies.  (ams_attend, 512 units of 4096 to 16384 positions: 348 us without, 321 so; 320 of 1000 to 16384, 128 queries: 884 and 620;
+// ams_recode, 1024 ragged units of up to 2048: 396 and 313.)
 __device__ __forceinline__ int turned_x(int first = 0) {
   const uint32_t y = blockIdx.y;
   return (int)((blockIdx.x - first + y + (y >> 1) + (y >> 2)) % (gridDim.x - first));

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void recode_kernel(RecodeArgs a) {
   int l, b, h;
   unit_coords(a.d, unit, l, b, h);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int blk = blockIdx.x * kWaves + wave;
+  const int blk = turned_x() * kWaves + wave;
   const int n = a.idx ? min(a.n_kept[unit], min(a.budget, a.d.t_max)) : seq_len(a.d, a.seq_lens, b);
   if (blk * kBlockRows >= n) return;
   const int32_t* idx = a.idx ? a.idx + (int64_t)unit * a.budget : nullptr;
