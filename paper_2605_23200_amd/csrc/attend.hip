@@ -476,10 +476,10 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
 __device__ __forceinline__ int splits_of(const AttendArgs& a, int T) { return max(1, (T + a.chunk - 1) / a.chunk); }
 
 // (largest logit, sum) of a query from its splits, for the LANES lanes that ask for it together; loads in batches, since a batch is a
-// latency.
+// latency (one unit of 131072 positions: 21 us a pass with half of this batch and of AHEAD below, 18 so).
 template <int LANES>
 __device__ __forceinline__ float2 joined_stats(const AttendArgs& a, int unit, int n, int n_splits, int lane) {
-  constexpr int BATCH = LANES == 64 ? 2 : 4;
+  constexpr int BATCH = 4;
   const float2* at = a.stats + ((int64_t)unit * a.d.N + n) * a.n_splits;
   float top = kLowest, sum = 0.f;
   for (int s0 = lane; s0 < n_splits; s0 += BATCH * LANES) {
@@ -506,7 +506,7 @@ __device__ __forceinline__ float2 joined_stats(const AttendArgs& a, int unit, in
 // and waves of the same channels together.
 template <bool BF16, int HD>
 __device__ __forceinline__ void join_splits(const AttendArgs& a, int unit, int n, int splits) {
-  constexpr int LANES = HD / 4, SIDE = 64 / LANES, AHEAD = 4;
+  constexpr int LANES = HD / 4, SIDE = 64 / LANES, AHEAD = 8;
   __shared__ __align__(16) float part[kWaves][HD];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const float2* stats = a.stats + ((int64_t)unit * a.d.N + n) * a.n_splits;
