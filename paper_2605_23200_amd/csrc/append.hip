@@ -120,23 +120,22 @@ __device__ __forceinline__ void normed_and_turned(const float (&x)[8], const flo
   }
   if constexpr (!ANY) {
     if (rot.mode == TURN_NONE) return;
+    // (channels behind the pairs are chosen as they are: turned by nothing, an infinity beside them would make them no number)
     M c[4], s[4];
+    bool turns[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      c[e] = cos_row[4 * i + e], s[e] = sin_row[4 * i + e];
-      if (4 * i + e >= rot.pairs) c[e] = (M)1, s[e] = (M)0;
-    }
+    for (int e = 0; e < 4; ++e) c[e] = cos_row[4 * i + e], s[e] = sin_row[4 * i + e], turns[e] = 4 * i + e < rot.pairs;
     if (rot.mode == TURN_HALVES) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const M p = y[e], q = y[4 + e];
-        y[e] = p * c[e] - q * s[e], y[4 + e] = q * c[e] + p * s[e];
+        const M p = y[e], q = y[4 + e], first = p * c[e] - q * s[e], second = q * c[e] + p * s[e];
+        y[e] = turns[e] ? first : p, y[4 + e] = turns[e] ? second : q;
       }
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const M p = y[2 * e], q = y[2 * e + 1];
-        y[2 * e] = p * c[e] - q * s[e], y[2 * e + 1] = q * c[e] + p * s[e];
+        const M p = y[2 * e], q = y[2 * e + 1], first = p * c[e] - q * s[e], second = q * c[e] + p * s[e];
+        y[2 * e] = turns[e] ? first : p, y[2 * e + 1] = turns[e] ? second : q;
       }
     }
   } else {
@@ -193,7 +192,7 @@ __device__ __forceinline__ void store_runs(char* row, int a, int b, const float 
 }
 
 // DST: element type of the cache; BF16: of the new rows (and of a cache of kv_dtype); ANY: rot.mode is TURN_ANY_HALVES, and no other
-// (a kernel with both takes 180 registers and 40 KB of LDS for int8, two workgroups on a CU; without, 146 and 24 KB, three).
+// (a kernel with both takes 180 registers and 40 KB of LDS for int8, two workgroups on a CU; without, 150 and 24 KB, three).
 template <int DST, bool BF16, int HD, bool ANY>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation rot) {
   constexpr int SRC = BF16 ? EL_BF16 : EL_F32, ES = kElBytes<SRC>;

@@ -378,6 +378,34 @@ def test_append_no_number_and_infinite():
     assert torch.equal(cache.t["k_scale"][0, 0, :, 0], scales["k"][0, 0, :, 0])
 
 
+@pytest.mark.parametrize("layout", [B.ROPE_HALF, B.ROPE_INTERLEAVED])
+@pytest.mark.parametrize("D,rot", [(128, 64), (128, 8), (128, 2), (128, 90), (64, 32), (64, 6)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_channels_that_do_not_rotate_pass_as_they_are(layout, D, rot, dtype):
+    """Behind rot_dim (no norm): infinities and NaN stay where they are and change nothing beside them, zeros keep their sign."""
+    H, G, n_new, rows = 2, 2, 5, ROWS[dtype]
+    gen = torch.Generator().manual_seed(rot)
+    x = torch.randn((1, 1, n_new, (G + 2) * H, D), generator=gen)
+    odd = torch.tensor([math.inf, -math.inf, math.nan, -0.0, 0.0])
+    places = torch.randperm(D - rot, generator=gen)[:min(D - rot, 20)] + rot
+    x[..., places] = odd[torch.randint(0, 5, x.shape[:-1] + (len(places),), generator=gen)]
+    x = x.to(rows)
+    cache = HostCache(dtype, (1, 1, H, D), 32)
+    view, dev = cache.upload(), x.to(DEV)
+    q_out = torch.zeros((1, 1, H * G, n_new, D), dtype=rows, device=DEV)
+    p = params((1, 1, H, D), 32, group=G, dtype=dtype)
+    B.ams_append(p, dev[..., :G * H, :], dev[..., G * H:(G + 1) * H, :], dev[..., (G + 1) * H:, :], None, None, 0.0,
+                 B.make_rope(rot, layout=layout, gain=1.25), lens_dev([777]), lens_dev([3]), q_out, view)
+    cache.download()
+    got = torch.cat([q_out[0, 0].cpu(), cache.t["k"][0, 0, :, 3:3 + n_new]]).transpose(0, 1)     # [token, query and key heads, D]
+    want = x[0, 0, :, :(G + 1) * H]
+    a, b = got[..., rot:].float(), want[..., rot:].float()
+    assert torch.equal(torch.isnan(a), torch.isnan(b))
+    there = ~torch.isnan(b)
+    assert torch.equal(a[there].view(torch.int32), b[there].view(torch.int32))
+    assert torch.isfinite(got[..., :rot].float()).all()
+
+
 # ---- ams_attend -------------------------------------------------------------------------------------------------
 
 def _attend_reference(q, k, v, W, causal):
