@@ -306,8 +306,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
       const bool number = need == need && had == had;
       const float scale = number ? fmaxf(need, had) : __uint_as_float(0x7FC00000u);
       const float inverse = scale_inverse(scale);
-      if (old > 0 && scale > had) {  // the rows that were there, rounded again
-        const float ratio = had * inverse;
+      if (old > 0 && !(scale == had)) {  // the rows that were there, rounded again; codes of 0 under a scale that is no number
+        const float ratio = number ? had * inverse : 0.f;
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
           const int r = p * ROWS + r0;

@@ -406,6 +406,33 @@ def test_append_channels_that_do_not_rotate_pass_as_they_are(layout, D, rot, dty
     assert torch.isfinite(got[..., :rot].float()).all()
 
 
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("paged", [False, True])
+def test_append_codes_of_a_block_that_turns_nan_are_zero(kind, paged):
+    """Those of the rows that the block held before too; rows behind the last and other blocks stay as they are."""
+    shape = (1, 1, 2, 64)
+    cache = _filled(kind, shape, 64, [20], paged, 0)
+    before = _At(cache, {n: t.clone() for n, t in cache.t.items()})
+    before_block = HostCache.block.__get__(before)
+    k, v = (torch.ones((1, 1, 1, 2, 64), dtype=torch.bfloat16) for _ in range(2))
+    k[0, 0, 0, 1, 3], v[0, 0, 0, 0, 0] = math.inf, math.nan
+    view, lens, p = cache.upload(), lens_dev([20]), params(shape, 64)
+    for new in range(2):                                # the row that is no number, then an ordinary one behind it
+        B.ams_append(p, None, k.to(DEV), v.to(DEV), None, None, 0.0, None, None, lens + new, None, view)
+        cache.download()
+        for name, h in (("k", 0), ("k", 1), ("v", 0), ("v", 1)):
+            rows, at = cache.block(name, 0, 0, h, 1)
+            was, _ = before_block(name, 0, 0, h, 1)
+            same_bits(rows[5 + new:], was[5 + new:], "rows behind the last")
+            if (name, h) in (("k", 1), ("v", 0)):
+                assert math.isnan(float(cache.t[name + "_scale"][at])) and not rows[:5 + new].view(torch.uint8).any(), (name, h, new)
+            else:
+                assert float(cache.t[name + "_scale"][at]) == float(before.t[name + "_scale"][at])
+                same_bits(rows[:4], was[:4])
+            same_bits(cache.block(name, 0, 0, h, 0)[0], before_block(name, 0, 0, h, 0)[0])
+        k, v = torch.ones_like(k), torch.ones_like(v)
+
+
 # ---- ams_attend -------------------------------------------------------------------------------------------------
 
 def _attend_reference(q, k, v, W, causal):
