@@ -279,11 +279,12 @@ def _own(s):
         else:
             B.ams_recode(h["p"], h["cache"], s["lens"], h["to"])
         if "back" in h:
-            B.ams_recode(h["p_back"], h["to"], h["lens_back"], h["back"])
+            B.ams_recode(h["p_back"], h["to"], h["kept"] if case["keep"] else s["lens"], h["back"])
         return _recoded(s)
-    B.ams_evict(h["p"], h["cache"], s["lens"], s["weights"], h["to"], s["weights_out"], s["idx"], s["n_kept"], h["ws"])
+    B.ams_evict(h["p"], h["cache"], s["lens"], s["weights"], h["to"], s["weights_out"], s["idx"], s["n_kept"], h["ws"],
+                h["kept"])
     if "back" in h:
-        B.ams_recode(h["p_back"], h["to"], h["lens_back"], h["back"])
+        B.ams_recode(h["p_back"], h["to"], h["kept"], h["back"])
     return dict(_recoded(s), idx=s["idx"], n_kept=s["n_kept"], weights=s["weights_out"])
 
 
@@ -308,12 +309,13 @@ def _handle(B, s):
     if kind == "evict":
         h["ws"] = torch.empty(B.ams_evict_workspace_bytes(h["p"]), dtype=torch.uint8, device=DEVICE)
     if kind in ("recode", "evict"):
+        # rows per sequence of what is written: what a gather is asked for; an eviction says it anew every time
+        h["kept"] = torch.full((case["batch"],), kept, dtype=torch.int32, device=DEVICE)
         h["to"] = B.cache_view(s["to_k"], s["to_v"], s["to_k_scale"], s["to_v_scale"])
         if "back_k" in s:
             h["back"] = B.cache_view(s["back_k"], s["back_v"])
             back = dict(common, kv_dtype=B.F32 if s["back_k"].dtype == torch.float32 else B.BF16)
             h["p_back"] = B.make_params(t_max=kept, budget=kept, **back)
-            h["lens_back"] = s["lens"].clamp(max=kept)
     return h
 
 
