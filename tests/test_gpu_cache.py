@@ -8,7 +8,9 @@ attend: a logit is a sum of D exact products in fp32 on the matrix cores: at mos
 2^-24 of the sum of magnitudes A = sum_d |q_d k_d| / sqrt(D), times the scale (2 more): err_s = 16 * 2^-24 * A, plus the subtraction of
 the largest and 2^x to an ulp of its own (2^-23 each way, of |s| up to 2 A): a probability is off by err_p = 2 err_s + 2^-21 relative,
 its normalisation included.  Probabilities enter the second product with 16 bits (2^-16 with rounding of both terms), fp32: 24 (2^-23)."""
+import importlib.util
 import math
+import os
 
 import numpy as np
 import pytest
@@ -1070,6 +1072,35 @@ def test_captured_calls_follow_the_lengths(W, T):
             for name in captured[k]:
                 same_bits(captured[k][name], eager[k][name], f"replay {replay}: {k} {name}")
         assert captured["lens_out"].tolist() == [min(x, budget) for x in n]
+
+
+def _measured():
+    """perf/operators.py as a module."""
+    spec = importlib.util.spec_from_file_location("operators", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "perf", "operators.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    m.own = True
+    return m
+
+
+@pytest.mark.parametrize("kind,kw", [("evict", dict(budget=150, sink=4, last=8, paged=True)), ("recode", dict(keep=0))])
+def test_measured_passes_follow_the_lengths(kind, kw):
+    """Lengths updated in place between two passes: what is read back goes by them, and rows behind them are left as they were."""
+    m = _measured()
+    case = m._case("", kind, layers=2, batch=2, heads=2, group=2, dim=64, code="int8", length=300, **kw)
+    s = m.prepare(case, 1)
+    m.run(s)
+    lens = [40, 123]
+    s["lens"].copy_(torch.tensor(lens, dtype=torch.int32))
+    s["back_k"].fill_(3.0)
+    s["back_v"].fill_(3.0)
+    out = m.run(s)
+    for name in ("k", "v"):
+        scale = s["to_" + name + "_scale"].repeat_interleave(BLOCK, -1)[..., :s["to_" + name].shape[3], None]
+        want = (s["to_" + name].float() * scale).to(out[name].dtype)
+        for b, n in enumerate(lens):
+            same_bits(out[name][:, b, :, :n].contiguous(), want[:, b, :, :n].contiguous(), f"{name} {b}")
+            assert (out[name][:, b, :, n:] == 3.0).all(), (name, b)
 
 
 def test_two_streams_at_once():
