@@ -11,6 +11,7 @@ its normalisation included.  Probabilities enter the second product with 16 bits
 import importlib.util
 import math
 import os
+import re
 
 import numpy as np
 import pytest
@@ -1072,6 +1073,31 @@ def test_captured_calls_follow_the_lengths(W, T):
             for name in captured[k]:
                 same_bits(captured[k][name], eager[k][name], f"replay {replay}: {k} {name}")
         assert captured["lens_out"].tolist() == [min(x, budget) for x in n]
+
+
+def test_the_loop_of_the_readme():
+    """As it stands there, over enough tokens for one eviction and two more: the lengths, and the newest rows in their places."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "README.md")) as f:
+        code, = [c for c in re.findall(r"```python\n(.*?)```", f.read(), re.S) if "ams_evict" in c]
+    Bt, H, G, D, steps = 2, 2, 3, 64, 130
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    r = lambda *s: torch.randn(s, device=DEV, generator=gen).to(torch.bfloat16)
+    rows = r(steps, 1, Bt, 1, (G + 2) * H, D)
+    ns = dict(torch=torch, B=B, Bt=Bt, H=H, G=G, D=D, K_out=r(1, Bt, H, 2048, D), V_out=r(1, Bt, H, 2048, D), lens=lens_dev([2048, 1000]),
+              idx=torch.zeros((Bt * H, 2048), dtype=torch.int32, device=DEV), n_kept=torch.zeros(Bt * H, dtype=torch.int32, device=DEV),
+              tokens=[(x[..., :G * H, :], x[..., G * H:(G + 1) * H, :], x[..., (G + 1) * H:, :]) for x in rows], q_norm=None, k_norm=None,
+              positions=lens_dev([9000, 9000]), q_rows=r(1, Bt, G * H, 1, D), out=r(1, Bt, G * H, 1, D), lse=torch.zeros((1, Bt, G * H, 1), device=DEV))
+    exec(code, ns)
+    assert ns["lens"].tolist() == [2050, 1130] and ns["positions"].tolist() == [9130, 9130]
+    _, v, _, v_scale = ns["cache"].tensors
+    for b, n in enumerate(ns["lens"].tolist()):         # the last 32 of the eviction and the two behind it
+        got = (v[0, b].float() * v_scale[0, b].repeat_interleave(BLOCK, -1)[..., None])[:, n - 34:n]
+        want = rows[-34:, 0, b, 0, (G + 1) * H:].float().transpose(0, 1)
+        # rounded to four bits at most three times (a scale that grows, an eviction), or by half a step of the smallest codes
+        assert ((got - want).abs() <= 3 * 2.0 ** -4 * want.abs() + 3 * 2.0 ** -10 * v_scale[0, b].max()).all()
+    assert (ns["weights"][:H, 2050:] == 0).all() and (ns["weights"][:H, 2049] > 0).all()
+    assert torch.isfinite(ns["out"].float()).all() and torch.isfinite(ns["lse"]).all()
 
 
 def _measured():
