@@ -10,7 +10,11 @@
 // 131072 positions of which 4096 stay: 316 us with digits of the whole row from one workgroup, 112 with a sample and one
 // walk, 53 now): a sample of the row says between which two values the wanted one lies, then many workgroups mark what is above
 // and what is between.  The digits are those of what is between.  The sample is wrong once in some thousand rows; the counts
-// show it, and the digits of the whole row decide.
+// show it, and the digits of the whole row decide.  So they do where more than 8192 positions lie between two different values: many
+// equal weights, and the wanted one so near their first or last that the values take in the others (zeros under a high budget), or equal
+// largest ones under a budget so small that the upper value is infinite.  One workgroup then walks the row up to four times (96
+// rows of up to 131072: this launch 223 us against 23 with half of the weights equal to the largest and 300 kept; 96 rows of 131072, 60000
+// kept, zeros from about there on: 298 against 95).
 #include "cache.h"
 
 namespace ams {

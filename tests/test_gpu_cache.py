@@ -864,6 +864,45 @@ def _evict_lists(w, lens, D, rules):
                 assert (out[u, kept:T] == 0).all() and (out[u, T:] == -5).all()
 
 
+def _sampled(T, n_sink, n_last):
+    """Positions that the sample of a long row looks at: 1024 runs of four over the candidates."""
+    n = T - n_sink - n_last
+    runs = n_sink + np.arange(1024, dtype=np.int64) * (n - 4) // 1024
+    return (runs[:, None] + np.arange(4)).reshape(-1)
+
+
+@pytest.mark.parametrize("budget,n_sink,n_last", [(25000, 4, 32), (20000, 0, 0), (30001, 16, 1)])
+def test_evict_long_rows_whose_sample_is_of_another_kind(budget, n_sink, n_last):
+    """Ordinary numbers where the sample misses: all that it sees is below, or above, the weight that is wanted."""
+    T = 50000
+    rng = np.random.default_rng(budget)
+    seen = _sampled(T, n_sink, n_last)
+    w = (1 + rng.random((3, T + 3))).astype(np.float32)
+    w[0, seen] -= 1                                     # its largest is below every other
+    w[1, seen] += 1
+    w[2] = np.where(np.isin(np.arange(T + 3), seen), rng.standard_normal(T + 3) * 1e-3, np.exp(rng.standard_normal(T + 3)))
+    middle = np.arange(n_sink, T - n_last)
+    need = budget - n_sink - n_last
+    for u, below in ((0, True), (1, False)):            # neither bound can then hold the wanted weight
+        wanted = np.sort(w[u, middle])[-need]
+        assert (w[u, seen].max() < wanted) if below else (w[u, seen].min() > wanted)
+    _evict_lists(w, [T] * 3, 64, ((budget, n_sink, n_last),))
+
+
+@pytest.mark.parametrize("T", [50000, 262144])
+def test_evict_long_rows_of_many_equal_weights_at_a_bound(T):
+    """More equal ones than are held between two different bounds: zeros under a high budget, a ceiling over a small one; on
+    both sides of the budgets at which the equal ones begin and end, and where both bounds are the equal weight."""
+    rng = np.random.default_rng(T)
+    w = rng.random((4, T + 3)).astype(np.float32) + np.float32(0.5)
+    many = rng.permutation(T)
+    w[0, many[:T * 6 // 10]] = 0
+    w[1, many[:T * 6 // 10]] = 5
+    w[2, many[:T // 2]] = np.where(rng.random(T // 2) < 0.5, -0.0, 0.0)
+    w[3, many[:T // 2]], w[3, many[T // 2:T * 9 // 10]] = 3, 0.25
+    _evict_lists(w, [T, T, T - 5, T], 64, ((300, 0, 0), (T * 4 // 10 - 50, 4, 32), (T * 4 // 10 + 90, 4, 32), (T // 2, 0, 1), (T * 9 // 10, 2, 2)))
+
+
 # ---- together ---------------------------------------------------------------------------------------------------
 
 def _loop_state(kind, steps, seed=0, paged=False):
