@@ -62,6 +62,24 @@ def test_bad_sizes(field, value, status):
     assert B.ams_attend_workspace_bytes(p) == 0 and B.ams_evict_workspace_bytes(p) == 0
 
 
+@pytest.mark.parametrize("t_max", [(1 << 30) + 1, (1 << 31) - 1])
+def test_lengths_beyond_the_kernels_positions(t_max):
+    """Positions are 32-bit numbers with room above them: longer caches are refused whatever the rows and strides hold."""
+    p = _p(t_max=t_max, t_stride=t_max, budget=200)
+    src, dst = _dense(cap=t_max), _dense(base=1 << 20, cap=t_max)
+    assert _attend(p, src) == B.ERR_UNSUPPORTED and _append(p, src, _tokens()) == B.ERR_UNSUPPORTED
+    assert _recode(p, src, dst) == B.ERR_UNSUPPORTED and _evict(p, src, dst) == B.ERR_UNSUPPORTED
+    assert B.ams_attend_workspace_bytes(p) == 0 and B.ams_evict_workspace_bytes(p) == 0
+    p = _p(t_max=1 << 30, t_stride=1 << 30)             # the longest
+    assert B.ams_attend_workspace_bytes(p) > 0 and B.ams_evict_workspace_bytes(p) > 0
+    assert _attend(p, _dense(cap=1 << 30), n=0) == B.ERR_WORKSPACE_TOO_SMALL
+
+
+def test_a_stride_shorter_than_the_row():
+    p = _p(t_max=1000, t_stride=999)
+    assert _attend(p, _dense()) == B.ERR_INVALID_ARG and _evict(p, _dense(), _dense(base=1 << 20)) == B.ERR_INVALID_ARG
+
+
 @pytest.mark.parametrize("cache,status", [
     (_dense(base=None), B.ERR_INVALID_ARG), (_dense(base=PTR + 8), B.ERR_INVALID_ARG), (_dense(cap=999), B.ERR_INVALID_ARG),
     (_dense(k_scale=None), B.ERR_INVALID_ARG), (_dense(v_scale=None), B.ERR_INVALID_ARG), (_dense(dtype=9), B.ERR_INVALID_ARG),
