@@ -332,7 +332,7 @@ int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t
  * (AMS_INT8) or 448 (AMS_E4M3): 0 for a = 0, NaN for a value that is infinite or no number (the whole
  * block is NaN then, its codes are 0), else 2^max(e, -120) with the least e for which a <= M * 2^e.  The
  * code is the nearest to value / scale, of two equally near ones the even one.  Powers of two: the
- * quotient is exact, every value of the cache is a bf16 number, and a scale that grows when rows are
+ * quotient is exact, every value of the cache is a bf16 number (for magnitudes below 2^127), and a scale that grows when rows are
  * appended costs the rows that are there at most half a step each time, of steps that at least double:
  * together less than one step of the final scale.  The readers take any finite scale.  Codes of
  * AMS_E4M3 that are no number are not written by the library; a caller's own make the sums they enter NaN.
@@ -359,7 +359,8 @@ typedef enum {
   AMS_ROPE_LINEAR = 1,  /* f_i / factor                                                                         */
   AMS_ROPE_BASE = 2,    /* with base * factor^(rot_dim / (rot_dim - 2)) for base; rot_dim > 2                   */
   AMS_ROPE_BY_PARTS = 3 /* f_i * (c + (1 - c) / factor), c = clamp((r - slow) / (fast - slow), 0, 1),
-                           r = original_len * f_i / (2 pi): the turns over the original context                 */
+                           r = original_len * f_i / (2 pi): the turns over the original context.  (Checkpoints whose code
+                           ramps over the index i instead: any other frequencies go straight into ams_rope.freq.)  */
 } ams_rope_scaling;
 typedef struct {
   int32_t layout;  /* ams_rope_layout                                                                     */
@@ -391,8 +392,8 @@ typedef struct {
  * ams_append - n_new tokens behind the seq_lens[b] rows of every sequence, in one pass: every query and key is normalised
  * over its head (x / sqrt(mean(x^2) + norm_eps) * weight; left out without a weight), then rotated, keys and values are
  * written to rows seq_lens[b] .. of the cache and the queries to q_out in the layout of ams_score and ams_attend.
- * The angles are formed in 64 bits and reduced there; what is written is rounded once (keys that go to 8 bits are normalised and
- * rotated in 64 bits).  Of p: the sizes, kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are
+ * The angles are formed in 64 bits and reduced there.  Queries and rows of kv_dtype are normalised and rotated in 32 bits (a norm's
+ * squares have to fit: magnitudes of up to 2^60) and rounded once to kv_dtype, keys that go to 8 bits in 64 bits.  Of p: the sizes, kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are
  * not written (a full sequence takes nothing), so seq_lens[b] = t_max leaves a sequence of a padded batch out.
  * A block of an 8-bit cache that already holds rows takes the larger of its scale and that of the new rows; where it
  * grows the rows that are there are rounded again (theirs are codes that are numbers and a scale that is not negative).  A block that
