@@ -332,9 +332,9 @@ int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t
  * (AMS_INT8) or 448 (AMS_E4M3): 0 for a = 0, NaN for a value that is infinite or no number (the whole
  * block is NaN then, its codes are 0), else 2^max(e, -120) with the least e for which a <= M * 2^e.  The
  * code is the nearest to value / scale, of two equally near ones the even one.  Powers of two: the
- * quotient is exact, every value of the cache is a bf16 number (for magnitudes below 2^127), and a scale that grows when rows are
- * appended costs the rows that are there at most half a step each time, of steps that at least double:
- * together less than one step of the final scale.  The readers take any finite scale.  Codes of
+ * quotient is exact, every value of the cache is a bf16 number (for magnitudes below 2^127), and a scale
+ * that grows when rows are appended costs the rows that are there at most half a step each time, of steps
+ * that at least double: together less than one step of the final scale.  The readers take any finite scale.  Codes of
  * AMS_E4M3 that are no number are not written by the library; a caller's own make the sums they enter NaN.
  * A block table entry outside the pool is read as the nearest page and never written through.  Blocks
  * that a call writes belong to one (sequence, place in the table) alone.
@@ -393,8 +393,9 @@ typedef struct {
  * over its head (x / sqrt(mean(x^2) + norm_eps) * weight; left out without a weight), then rotated, keys and values are
  * written to rows seq_lens[b] .. of the cache and the queries to q_out in the layout of ams_score and ams_attend.
  * The angles are formed in 64 bits and reduced there.  Queries and rows of kv_dtype are normalised and rotated in 32 bits (a norm's
- * squares have to fit: magnitudes of up to 2^60) and rounded once to kv_dtype, keys that go to 8 bits in 64 bits.  Of p: the sizes, kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are
- * not written (a full sequence takes nothing), so seq_lens[b] = t_max leaves a sequence of a padded batch out.
+ * squares have to fit: magnitudes of up to 2^60) and rounded once to kv_dtype, keys that go to 8 bits in 64 bits.  Of p: the sizes,
+ * kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are not written (a full sequence takes
+ * nothing), so seq_lens[b] = t_max leaves a sequence of a padded batch out.
  * A block of an 8-bit cache that already holds rows takes the larger of its scale and that of the new rows; where it
  * grows the rows that are there are rounded again (theirs are codes that are numbers and a scale that is not negative).  A block that
  * the call begins takes nothing from its old scale.

@@ -15,7 +15,7 @@ SOURCES = ["ams_api.hip", "score.hip", "score_causal.hip", "score_last.hip", "sc
 
 # -ffp-contract=off: multiply-adds are fused only where the source says fmaf(), so that host-checkable
 # double arithmetic (quotas, normalisers) rounds exactly like plain C.
-# packed fp32 instructions are switched off for the test machines of machines.
+# Packed fp32 instructions are switched off: some of their forms have given wrong results on the machines used.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Wno-unknown-attributes",

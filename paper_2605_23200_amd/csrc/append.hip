@@ -10,7 +10,7 @@
 // cosines and sines out of LDS, took 35 us for 2036 tokens of 48 heads against 23: every read hit the same banks.)  Halves that are no
 // multiple of four channels find the other channel in LDS.
 // What bounds it: a launch and its chain of latencies for single tokens (5 us for one, 7 for 64 sequences); 64-bit arithmetic of the
-// keys for long pieces (17 us for 2036 tokens of 48 heads to 8 bits, of 10 that the bytes take; 27 for 4096 tokens to bf16, 2048 each).
+// keys for long pieces (17 us for 2036 tokens of 48 heads to 8 bits, of 10 that the bytes take; 25 for 4096 tokens to bf16, 2048 each).
 // Angles: position * (frequency / 2 pi) in 64 bits, whole turns taken off there: at position 10^6 fp32 would be off by 0.06 rad.
 // Keys that go to 8 bits are normalised and rotated in 64 bits: a code changes by a whole step where the value
 // crosses the middle between two, and fp32 takes about one key element in a million across.

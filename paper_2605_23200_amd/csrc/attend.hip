@@ -15,8 +15,9 @@
 // What bounds it: the bytes of K and V.  512 paged units of 4096 to 16384 positions: 288 us, 5.1 TB/s with the logits it writes (without
 // weights, 256 dense units of 16384: 5.5 TB/s); 4 units of 131072: 33 us of 28 at the rate of a copy.  It reads that fast because
 // tables and scales come through the scalar cache, a name of a page two steps before its codes (vector loads of them: 507 us), and
-// because no load is under a condition.  More than 32 queries are bound by instructions: 440 of the vector ALU and 48 products for 32
-// positions and 32 queries, 44 us for 8 units of 32768 positions and 128 queries.  (Sharing the conversions of four waves through
+// because no load is under a condition.  More than 32 queries are bound by what follows from one another within a step: 436 vector
+// instructions and 48 products for 32 positions and 32 queries, 44 us for 8 units of 32768 positions and 128 queries, in which the
+// vector ALU is active for 51 % and the matrix cores for 21 %.  (Sharing the conversions of four waves through
 // LDS: 52; the masks as a variant of the step: 44, but 128 against 120 for 64 units and 32 queries.)
 //
 // Weights: with up to 16 queries the logits go to scratch (4 N bytes a position, written and read once, against 2 D of K and V)

@@ -6,7 +6,7 @@
 // moves once; no LDS, no barrier.  Memory is the bound: what a gathered row waits for (index, page, then scale and row) is a
 // chain of latencies, so a wave starts all rows of K and V of its block before it looks at the first: 256 units, 2048 of
 // 2176 rows, 8 bits to 8 bits: 94 us with a wave for K and one for V that loaded row by row, 52 so (5.2 TB/s); 2048 of 32768 bf16 rows
-// to 8 bits: 96 and 83 (4.9 TB/s); 96 paged units, rows of 128 bytes scattered over a pool: 51 (4.1 TB/s).  Rows of kv_dtype as they
+// to 8 bits: 96 and 83 (4.9 TB/s); 96 paged units, rows of 128 bytes scattered over a pool: 52 (3.9 TB/s).  Rows of kv_dtype as they
 // are: an eviction of 256 units to 2048 of 32768 takes 162 us, with a copy that went row by row 164.
 #include "cache.h"
 
