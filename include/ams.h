@@ -50,7 +50,9 @@ typedef enum {
   AMS_F32 = 0,
   AMS_BF16 = 1,
   AMS_INT8 = 2, /* ams_cache only: one-byte codes with a scale per block, see there      */
-  AMS_E4M3 = 3  /* ams_cache only: the 8-bit float of 4 exponent and 3 mantissa bits      */
+  AMS_E4M3 = 3, /* ams_cache only: the 8-bit float of 4 exponent and 3 mantissa bits      */
+  AMS_E2M1 = 4  /* ams_cache only: the 4-bit float of 2 exponent and 1 mantissa bit, two a byte, with a scale byte
+                   per row and 32 channels, see there */
 } ams_dtype;
 
 /* Plug-in base scorer g (Sec. 3.3 "In-Segment Selection with a Plug-and-Play
@@ -318,12 +320,12 @@ int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t
                       int32_t* idx, int32_t* n_kept, void* ws, size_t ws_bytes, void* stream);
 
 /*
- * ---- Between two events: new rows, attention, eviction, caches in 8 bits ----
+ * ---- Between two events: new rows, attention, eviction, caches in 8 and 4 bits, pages ----
  *
  * ams_cache - a cache of any element type.  kv_dtype rows (dtype == p->kv_dtype; the scales are
  * ignored), or one-byte codes with one fp32 scale for K and one for V per BLOCK: 16 consecutive
- * positions (16 j .. 16 j + 15) of one (layer, sequence, KV head), which is a page of the paged layout.
- * A row's values are code * scale.
+ * positions (16 j .. 16 j + 15) of one (layer, sequence, KV head), which is a page of the paged layout; or codes of
+ * 4 bits (AMS_E2M1, further down).  A row's values are code * scale.
  *   kv        k, v: kv_dtype rows, or codes in the same layouts, one byte each; 16-byte aligned;
  *             paged: n_slots a multiple of 16 for codes
  *   k_scale, v_scale  [dev] fp32; dense [layers, batch, kv_heads, ceil(t_capacity / 16)], paged
@@ -336,6 +338,14 @@ int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t
  * that grows when rows are appended costs the rows that are there at most half a step each time, of steps
  * that at least double: together less than one step of the final scale.  The readers take any finite scale.  Codes of
  * AMS_E4M3 that are no number are not written by the library; a caller's own make the sums they enter NaN.
+ * AMS_E2M1: floats of one sign, two exponent and one mantissa bit (magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6), two a byte, the even
+ * channel in the low half; rows of head_dim / 2 bytes in the same layouts.  Every row has a scale byte x for each 32 of its channels:
+ * 2^(x - 127), 255: all 32 are no number.  k_scale and v_scale point to bytes (16-byte aligned): those of a block lie together, its 16
+ * positions for the first 32 channels, then for the next: dense [layers, batch, kv_heads, ceil(t_capacity / 16), head_dim / 32, 16],
+ * paged [layers, n_slots / 16, kv_heads, head_dim / 32, 16].  The writers' scale is the least power of two from 2^-120 on that takes the
+ * largest magnitude of the 32 to 7 or less (0 for zeros, 255 for a value that is infinite or no number, both with codes of 0), the code the
+ * nearest to value / scale, of two equally near ones the even one: no code is off by more than half of the steps between 4 and 6.  A row's
+ * codes depend on that row alone: what is in the cache is never rounded again.  The readers take any byte (0 is 2^-127).
  * A block table entry outside the pool is read as the nearest page and never written through.  Blocks
  * that a call writes belong to one (sequence, place in the table) alone.
  * Outputs of the calls below overlap neither inputs nor one another unless it says so; calls that overlap in
@@ -344,7 +354,7 @@ int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t
 typedef struct {
   ams_kv_view kv;
   int32_t dtype;  /* ams_dtype of k and v */
-  float* k_scale;
+  float* k_scale; /* AMS_E2M1: bytes */
   float* v_scale;
 } ams_cache;
 
@@ -393,7 +403,7 @@ typedef struct {
  * over its head (x / sqrt(mean(x^2) + norm_eps) * weight; left out without a weight), then rotated, keys and values are
  * written to rows seq_lens[b] .. of the cache and the queries to q_out in the layout of ams_score and ams_attend.
  * The angles are formed in 64 bits and reduced there.  Queries and rows of kv_dtype are normalised and rotated in 32 bits (a norm's
- * squares have to fit: magnitudes of up to 2^60) and rounded once to kv_dtype, keys that go to 8 bits in 64 bits.  Of p: the sizes,
+ * squares have to fit: magnitudes of up to 2^60) and rounded once to kv_dtype, keys that go to 8 or 4 bits in 64 bits.  Of p: the sizes,
  * kv_dtype and t_max, the upper bound of the lengths AFTER the call; rows from t_max on are not written (a full sequence takes
  * nothing), so seq_lens[b] = t_max leaves a sequence of a padded batch out.
  * A block of an 8-bit cache that already holds rows takes the larger of its scale and that of the new rows; where it
@@ -412,13 +422,13 @@ size_t ams_attend_workspace_bytes(const ams_params* p);
 size_t ams_evict_workspace_bytes(const ams_params* p);
 
 /*
- * ams_attend - attention of the query window over a cache in 8 bits, and the weights that its positions received.
+ * ams_attend - attention of the query window over a cache in 8 or 4 bits, and the weights that its positions received.
  *   s[n][t] = q_n . k_t / sqrt(D), p = softmax over the positions that n sees, out_n = sum_t p[n][t] v_t,
  *   lse_n = ln sum_t exp(s[n][t]),  weights_out[t] = weights_in[t] + sum_n p[n][t]   (n: the unit's G * W queries)
  * p->causal == 0: every query sees 0 .. T-1; 1: query w sits at T-W+w and sees 0 .. T-W+w.  A query that sees nothing
  * (T = 0; before position 0) has out 0 and lse -inf and adds no weight.
  * Of p: the sizes, kv_dtype (of q and out), causal, t_max, t_stride; group * window <= 256 (AMS_ERR_UNSUPPORTED).
- *   src   AMS_INT8 or AMS_E4M3 (AMS_ERR_UNSUPPORTED otherwise)
+ *   src   AMS_INT8, AMS_E4M3 or AMS_E2M1 (AMS_ERR_UNSUPPORTED otherwise)
  *   q     [dev] [layers, batch, kv_heads * group, window, head_dim] kv_dtype; out likewise, written
  *   lse   [dev] fp32 [layers, batch, kv_heads * group, window], or NULL
  *   weights_in, weights_out  [dev] fp32 [units, t_stride]; entries 0 .. T-1 read and written, the others left as they are; weights_in
@@ -433,11 +443,13 @@ int ams_attend(const ams_params* p, const ams_cache* src, const int32_t* seq_len
                const float* weights_in, float* weights_out, void* ws, size_t ws_bytes, void* stream);
 
 /*
- * ams_recode - ams_compact between caches of different element types: rows of kv_dtype to 8 bits, 8 bits to rows, 8 bits to 8 bits.
+ * ams_recode - ams_compact between caches of different element types: rows of kv_dtype to 8 or 4 bits, these to rows, and among
+ * themselves.
  *   idx != NULL: row j < n_kept[unit] of the destination is row idx[unit * budget + j] of the source (an index
  *         outside [0, t_max) gives a row of zeros), credit as in ams_compact; seq_lens is not read
  *   idx == NULL: rows 0 .. seq_lens[b]-1 in place order; n_kept, credit_src and credit_dst are not used
- * Every block takes a scale of its own (ams_cache); rows behind the last one are left as they are.  src and
+ * Every block (in 4 bits every 32 channels of a row) takes a scale of its own (ams_cache); 4 bits to 4 bits: codes and scales as they
+ * are.  Rows behind the last one, and in 4 bits their scales, are left as they are.  src and
  * dst must not overlap.  Two caches of kv_dtype: AMS_ERR_UNSUPPORTED (ams_compact does that).
  */
 int ams_recode(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const int32_t* idx, const int32_t* n_kept,
@@ -456,6 +468,36 @@ int ams_recode(const ams_params* p, const ams_cache* src, const int32_t* seq_len
  */
 int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const float* weights, const ams_cache* dst,
               float* weights_out, int32_t* idx, int32_t* n_kept, int32_t* lens_out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ams_assign_pages - block tables, slots of new tokens and the free pages of a pool, from the rows that every sequence has and is to
+ * have.  A pool's free pages are a ring: `count` names from ring[head] on, round the end of its n_pages places; state = {head, count}.  (A
+ * new pool: ring = 0 .. n_pages - 1, state = {0, n_pages}.)
+ * With from = lens_from[b] and to = lens_to[b] a sequence keeps its first ceil(from / 16) pages; where to needs more, it takes them
+ * from the front of the ring, sequences in order, and where to needs fewer, those behind go to the end of the ring, in order of
+ * (sequence, place).  Pages that go back in a call are given out from the next call on.  A sequence that the free pages do not
+ * suffice for stays as it was, and so do those behind it that ask for pages; the others are served.
+ *   table, table_out  [dev] [batch, max_blocks_per_seq]; entries behind a sequence's pages are -1 in table_out and not read in table; may
+ *               be the same array
+ *   ring        [dev] [n_pages], updated; state, state_out [dev] [2], not the same array
+ *   lens_out    [dev] [batch] to, or from where the sequence is not served; NULL; not lens_from or lens_to
+ *   starts      [dev] [batch + 1]: the new tokens (max(to - from, 0)) of the sequences before b, or NULL
+ *   slots       [dev] [n_slots]: slots[starts[b] + i] = the pool's slot of position from + i of sequence b, page * 16 + position % 16, -1
+ *               for a sequence that is not served; -1 from the last token to n_slots; tokens beyond n_slots have none.  NULL with 0
+ * Of p: the sizes and t_max, the upper bound of the lengths; max_blocks_per_seq * 16 >= t_max, batch * t_max < 2^31
+ * (AMS_ERR_UNSUPPORTED).  One table serves all layers.  The names in ring and table are taken as they are.
+ */
+typedef struct {
+  const int32_t* table;
+  int32_t* table_out;
+  int32_t max_blocks_per_seq;
+  int32_t n_pages;
+  int32_t* ring;
+  const int32_t* state;
+  int32_t* state_out;
+} ams_pages;
+int ams_assign_pages(const ams_params* p, const ams_pages* x, const int32_t* lens_from, const int32_t* lens_to, int32_t* lens_out,
+                     int32_t* starts, int64_t* slots, int64_t n_slots, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libams.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE_TOO_SMALL, ERR_HIP = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
-INT8, E4M3 = 2, 3                     # element types of a cache only (cache_view)
+INT8, E4M3, E2M1 = 2, 3, 4            # element types of a cache only (cache_view)
 SCORER_LAST_QUERY, SCORER_MEAN_WINDOW, SCORER_KEYDIFF, SCORER_EXPECTED, SCORER_EXTERNAL = 0, 1, 2, 3, 4
 SCORER_EXPECTED_VNORM = 5
 SCORER_REDUNDANCY = 6
@@ -32,7 +32,7 @@ EXPORTS = ("ams_status_string", "ams_workspace_bytes", "ams_workspace_layout", "
            "ams_profile_end", "ams_debug_set_wait_limit", "ams_score",
            "ams_ema_update", "ams_mass_segment", "ams_mass_segment_static", "ams_select", "ams_compact",
            "ams_compress_step", "ams_rope_init", "ams_append", "ams_attend_workspace_bytes", "ams_attend", "ams_recode",
-           "ams_evict_workspace_bytes", "ams_evict")
+           "ams_evict_workspace_bytes", "ams_evict", "ams_assign_pages")
 
 
 class AmsError(RuntimeError):
@@ -83,6 +83,11 @@ class NewTokens(C.Structure):
                 ("positions", C.c_void_p), ("n_new", C.c_int32)]
 
 
+class Pages(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_out", C.c_void_p), ("max_blocks_per_seq", C.c_int32), ("n_pages", C.c_int32),
+                ("ring", C.c_void_p), ("state", C.c_void_p), ("state_out", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -114,6 +119,7 @@ def lib() -> C.CDLL:
         l.ams_attend.argtypes = [P, K, p, p, p, p, p, p, p, C.c_size_t, p]
         l.ams_recode.argtypes = [P, K, p, p, p, K, p, p, p]
         l.ams_evict.argtypes = [P, K, p, p, K, p, p, p, p, p, C.c_size_t, p]
+        l.ams_assign_pages.argtypes = [P, C.POINTER(Pages), p, p, p, p, p, C.c_int64, p]
         for name in EXPORTS[2:]:
             getattr(l, name).restype = C.c_int
         for name in ("ams_attend_workspace_bytes", "ams_evict_workspace_bytes"):
@@ -242,35 +248,38 @@ def ams_compress_step(p, src, seq_lens, q, credit, dst, credit_dst, idx, n_kept,
                                    ws.numel() * ws.element_size(), _stream(stream)), "ams_compress_step")
 
 
-# ---- between two events: new rows, attention, eviction, caches in 8 bits ----
+# ---- between two events: new rows, attention, eviction, caches in 8 and 4 bits, pages ----
 
-_CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: INT8, torch.float8_e4m3fn: E4M3}
-BLOCK = 16                             # positions that share a scale
+_CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: INT8, torch.float8_e4m3fn: E4M3, torch.uint8: E2M1,
+                 torch.float4_e2m1fn_x2: E2M1}
+BLOCK = 16                             # positions that share a scale (in 4 bits: whose scales lie together); a page
+MICRO = 32                             # channels of a row that share a scale in 4 bits
 
 
 def scale_shape(k: torch.Tensor):
-    """Shape of k_scale and v_scale of a cache whose keys have the shape of `k` (dense or paged)."""
-    if k.dim() == 5:
-        return tuple(k.shape[:3]) + (-(-k.shape[3] // BLOCK),)
-    return (k.shape[0], k.shape[1] // BLOCK, k.shape[2])
+    """Shape of k_scale and v_scale of a cache whose keys have the shape of `k` (dense or paged; in 4 bits two channels an element)."""
+    lead = tuple(k.shape[:3]) + (-(-k.shape[3] // BLOCK),) if k.dim() == 5 else (k.shape[0], k.shape[1] // BLOCK, k.shape[2])
+    return lead + (2 * k.shape[-1] // MICRO, BLOCK) if _CACHE_DTYPES.get(k.dtype) == E2M1 else lead
 
 
 def cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
                v_scale: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None) -> Cache:
-    """A cache of rows (bf16, fp32) or of codes (int8, float8_e4m3fn) with their scales: k, v [L, B, H, t_capacity, D], or, with a
-    block table (int32 [B, max_blocks]), pools [L, n_slots, H, D]."""
+    """A cache of rows (bf16, fp32) or of codes (int8, float8_e4m3fn; two a byte in uint8 or float4_e2m1fn_x2) with their scales: k, v
+    [L, B, H, t_capacity, D], or, with a block table (int32 [B, max_blocks]), pools [L, n_slots, H, D]; D / 2 bytes a row in 4 bits."""
     tensors = [t for t in (k, v, k_scale, v_scale, block_table) if t is not None]
     if any(not t.is_cuda or t.device != k.device for t in tensors):
         raise ValueError("a cache's tensors lie on one GPU")
     if any(not t.is_contiguous() for t in tensors):
         raise ValueError("contiguous tensor expected")
     if k.dtype not in _CACHE_DTYPES or k.dtype != v.dtype or k.shape != v.shape or k.dim() != (5 if block_table is None else 4):
-        raise ValueError("k and v: one shape, one element type of bf16, fp32, int8, float8_e4m3fn; five dimensions, paged four")
+        raise ValueError("k and v: one shape, one element type of bf16, fp32, int8, float8_e4m3fn, uint8, float4_e2m1fn_x2; "
+                         "five dimensions, paged four")
     dtype = _CACHE_DTYPES[k.dtype]
-    if dtype in (INT8, E4M3):
+    if dtype in (INT8, E4M3, E2M1):
+        kinds = (torch.uint8, torch.float8_e8m0fnu) if dtype == E2M1 else (torch.float32,)
         for t in (k_scale, v_scale):
-            if t is None or t.dtype != torch.float32 or tuple(t.shape) != scale_shape(k):
-                raise ValueError(f"fp32 scales of shape {scale_shape(k)} expected")
+            if t is None or t.dtype not in kinds or tuple(t.shape) != scale_shape(k):
+                raise ValueError(f"{' or '.join(str(t) for t in kinds)} scales of shape {scale_shape(k)} expected")
     elif k_scale is not None or v_scale is not None:
         raise ValueError("rows of bf16 or fp32 have no scales")
     if block_table is not None and (block_table.dtype != torch.int32 or block_table.dim() != 2):
@@ -279,7 +288,7 @@ def cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor]
     c = Cache(kv, dtype, k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None)
     c.tensors, c.index = tensors, k.get_device()
     c.lead = tuple(k.shape[:3]) if block_table is None else (k.shape[0], block_table.shape[0], k.shape[2])
-    c.head_dim = k.shape[-1]
+    c.head_dim = k.shape[-1] * (2 if dtype == E2M1 else 1)
     return c
 
 
@@ -394,6 +403,21 @@ def ams_evict(p, src, seq_lens, weights, dst, weights_out, idx, n_kept, ws, lens
             _arg(weights_out, torch.float32, p.units * p.t_stride, gpu, "weights_out"),
             _arg(idx, torch.int32, p.units * p.budget, gpu, "idx"), _arg(n_kept, torch.int32, p.units, gpu, "n_kept"),
             _arg(lens_out, torch.int32, p.batch, gpu, "lens_out"), _arg(ws, torch.uint8, 0, gpu, "ws"), ws.numel())
+
+
+def ams_assign_pages(p, lens_from, lens_to, table, table_out, ring, state, state_out, starts=None, slots=None, lens_out=None, stream=None):
+    """table, table_out int32 [batch, max_blocks] (may be one tensor), ring int32 [n_pages], state, state_out int32 [2], starts int32
+    [batch + 1], slots int64, any length."""
+    gpu, i32 = table.get_device(), torch.int32
+    if gpu < 0 or table.dim() != 2 or table.shape[0] != p.batch or table_out.shape != table.shape or ring.dim() != 1:
+        raise ValueError(f"block tables [{p.batch}, max_blocks] on a GPU and a ring of one dimension expected")
+    n = table.numel()
+    x = Pages(_arg(table, i32, n, gpu, "table"), _arg(table_out, i32, n, gpu, "table_out"), table.shape[1], ring.numel(),
+              _arg(ring, i32, 1, gpu, "ring"), _arg(state, i32, 2, gpu, "state"), _arg(state_out, i32, 2, gpu, "state_out"))
+    _launch((_lib or lib()).ams_assign_pages, "ams_assign_pages", gpu, stream, C.byref(p), C.byref(x),
+            _arg(lens_from, i32, p.batch, gpu, "lens_from"), _arg(lens_to, i32, p.batch, gpu, "lens_to"),
+            _arg(lens_out, i32, p.batch, gpu, "lens_out"), _arg(starts, i32, p.batch + 1, gpu, "starts"),
+            _arg(slots, torch.int64, 0, gpu, "slots"), slots.numel() if slots is not None else 0)
 
 
 @dataclass

@@ -11,7 +11,7 @@ LIB = os.path.join(PKG, "libams.so")
 OBJ_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["ams_api.hip", "score.hip", "score_causal.hip", "score_last.hip", "score_causal_last.hip", "score_keys.hip", "score_park.hip", "score_unit.hip", "mass_segment.hip", "select.hip", "compact.hip",
-           "cache_api.hip", "append.hip", "attend.hip", "recode.hip", "evict.hip"]
+           "cache_api.hip", "append.hip", "attend.hip", "attend_e2m1.hip", "recode.hip", "evict.hip", "pages.hip"]
 
 # -ffp-contract=off: multiply-adds are fused only where the source says fmaf(), so that host-checkable
 # double arithmetic (quotas, normalisers) rounds exactly like plain C.

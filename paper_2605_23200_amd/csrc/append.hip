@@ -190,6 +190,23 @@ __device__ __forceinline__ void store_runs(char* row, int a, int b, const float 
     *(uint32_t*)(row + a) = p.x, *(uint32_t*)(row + b) = p.y;
   }
 }
+// Two runs of four as codes of 4 bits; at[c]: bits of the largest magnitude among channels 4 c .. 4 c + 3 of the row (a stretch of LDS
+// of the row's lanes).  The lane whose run begins 32 channels writes their scale; scales: of the row, kBlockRows from one to the next.
+template <int HD>
+__device__ __forceinline__ void store_micro_runs(char* row, uint8_t* scales, int a, int b, const float (&x)[8], const uint32_t* at, bool real) {
+#pragma unroll
+  for (int run = 0; run < 2; ++run) {
+    const int d = run ? b : a;
+    const uint4* of = (const uint4*)(at + d / kMicroChannels * (kMicroChannels / 4));
+    const uint4 p = of[0], q = of[1];
+    const uint32_t byte = micro_scale(max(max(max(p.x, p.y), max(p.z, p.w)), max(max(q.x, q.y), max(q.z, q.w))));
+    const float inverse = micro_inverse(byte);
+    const uint32_t w = inverse == 0.f ? 0u : pack_four_bits(x[4 * run] * inverse, x[4 * run + 1] * inverse, x[4 * run + 2] * inverse, x[4 * run + 3] * inverse);
+    if (!real) continue;
+    *(uint16_t*)(row + d / 2) = (uint16_t)w;
+    if (d % kMicroChannels == 0) scales[d / kMicroChannels * kBlockRows] = (uint8_t)byte;
+  }
+}
 
 // DST: element type of the cache; BF16: of the new rows (and of a cache of kv_dtype); ANY: rot.mode is TURN_ANY_HALVES, and no other
 // (a kernel with both takes 180 registers and 40 KB of LDS for int8, two workgroups on a CU; without, 150 and 24 KB, three).
@@ -197,10 +214,11 @@ template <int DST, bool BF16, int HD, bool ANY>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation rot) {
   constexpr int SRC = BF16 ? EL_BF16 : EL_F32, ES = kElBytes<SRC>;
   constexpr int LANES = HD / 8, ROWS = 64 / LANES, PASSES = kBlockRows / ROWS;
-  constexpr bool PACK = kPacked<DST>;
+  constexpr bool PACK = kCodes<DST>;
   using M = std::conditional_t<PACK, double, float>;  // of keys
   __shared__ Turns<float> turns;
   __shared__ Turns<M> exact;  // (unused where M is float)
+  __shared__ __align__(16) uint32_t largest[kMicro<DST> ? kWaves : 1][kMicro<DST> ? PASSES : 1][kMicro<DST> ? ROWS : 1][HD / 4];
   __shared__ __align__(16) M exchange[ANY ? kWaves : 1][ANY ? ROWS : 1][ANY ? HD : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int b = blockIdx.y % a.d.B, l = blockIdx.y / a.d.B;
@@ -297,6 +315,26 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Rotation
         const int r = p * ROWS + r0;
         if (r < kept) store_runs<SRC>(to.row0 + (old + r) * to.stride, run_a, run_b, x[p]);
       }
+    } else if constexpr (kMicro<DST>) {  // every row has scales of its own: those that were there stay as they are
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's own stretch of LDS: its last readers are done
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        if (p * ROWS >= kept) break;
+        uint32_t ta = 0, tb = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ta = max(ta, __float_as_uint(x[p][e]) & 0x7FFFFFFFu), tb = max(tb, __float_as_uint(x[p][4 + e]) & 0x7FFFFFFFu);
+        largest[wave][p][r0][run_a / 4] = ta, largest[wave][p][r0][run_b / 4] = tb;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        if (p * ROWS >= kept) break;
+        const int r = p * ROWS + r0;
+        uint8_t* scales = (uint8_t*)dst.scale + to.scale * kMicroBytes<HD> + old + r;
+        store_micro_runs<HD>(to.row0 + (old + r) * to.stride, scales, run_a, run_b, x[p], largest[wave][p][r0], r < kept);
+      }
     } else {
       uint32_t top = 0;
 #pragma unroll
@@ -336,7 +374,7 @@ hipError_t launch(const AppendArgs& a, const Rotation& rot, hipStream_t s) {
   // Slices of the heads: one round of workgroups, three on a CU where keys are formed in 64 bits (their registers), else four.  2036
   // tokens of 48 heads to 8 bits: 20.0 us with 396 workgroups, 17.3 with 660, 21.9 with 924; 4096 tokens, bf16: 38.5 with 516, 25.3
   // with 1032, 29.5 with 1548.
-  const int slices = min(max(1, (kPacked<DST> ? 768 : 1024) / (int)min((int64_t)tiles * rows, (int64_t)1024)), div_up(tasks, kWaves));
+  const int slices = min(max(1, (kCodes<DST> ? 768 : 1024) / (int)min((int64_t)tiles * rows, (int64_t)1024)), div_up(tasks, kWaves));
   prof_mark("append", s);
   const dim3 grid(tiles, rows, slices);
   if (rot.mode == TURN_ANY_HALVES)
@@ -351,6 +389,7 @@ hipError_t launch_to(const AppendArgs& a, const Rotation& rot, int el, hipStream
   switch (el) {
     case EL_INT8: return launch<EL_INT8, BF16, HD>(a, rot, s);
     case EL_E4M3: return launch<EL_E4M3, BF16, HD>(a, rot, s);
+    case EL_E2M1: return launch<EL_E2M1, BF16, HD>(a, rot, s);
     default: return launch<BF16 ? EL_BF16 : EL_F32, BF16, HD>(a, rot, s);
   }
 }

@@ -11,16 +11,29 @@ namespace ams {
 constexpr int kBlockRows = 16;  // positions that share a scale; a page of the paged layout
 
 // Element types as the kernels are instantiated for them.
-enum { EL_F32 = AMS_F32, EL_BF16 = AMS_BF16, EL_INT8 = AMS_INT8, EL_E4M3 = AMS_E4M3 };
+enum { EL_F32 = AMS_F32, EL_BF16 = AMS_BF16, EL_INT8 = AMS_INT8, EL_E4M3 = AMS_E4M3, EL_E2M1 = AMS_E2M1 };
 template <int EL>
-constexpr bool kPacked = EL == EL_INT8 || EL == EL_E4M3;
+constexpr bool kPacked = EL == EL_INT8 || EL == EL_E4M3;  // 8 bits, a scale per block
+template <int EL>
+constexpr bool kMicro = EL == EL_E2M1;                    // 4 bits, a scale per 32 channels of a row
+template <int EL>
+constexpr bool kCodes = kPacked<EL> || kMicro<EL>;
 template <int EL>
 constexpr int kElBytes = EL == EL_F32 ? 4 : EL == EL_BF16 ? 2 : 1;
+template <int EL>
+constexpr int kEightBytes = kMicro<EL> ? 4 : 8 * kElBytes<EL>;  // of eight elements
+
+// Scales of 4 bits: bytes, those of a block together, its 16 positions for every 32 channels.
+constexpr int kMicroChannels = 32;
+template <int HD>
+constexpr int kMicroBytes = HD / kMicroChannels * kBlockRows;
+template <int HD>
+__device__ __forceinline__ uint32_t micro_at(int channel, int row) { return channel / kMicroChannels * kBlockRows + row; }
 
 // One of K / V of a cache.
 struct CacheDev {
   char* base;
-  float* scale;  // null for rows of kv_dtype
+  float* scale;  // null for rows of kv_dtype; bytes in 4 bits
   const int32_t* table;
   int64_t t_capacity;  // dense: rows per unit
   int64_t n_pages;     // paged: pages per layer
@@ -107,6 +120,35 @@ __device__ __forceinline__ void unpack_codes(uint32_t w, float (&x)[4]) {
     x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
     x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
   }
+}
+
+// Scale byte of 32 channels of 4 bits from the bits of their largest magnitude: the least power of two that takes it to 7 = 1.75 * 2^2 or
+// less.  (7 and not 6, the largest code: between 6 and 7 a value is as near to 6 as others of that binade may be to their codes.)
+__device__ __forceinline__ uint32_t micro_scale(uint32_t top) {
+  if (top == 0) return 0;
+  if (top >= 0x7F800000u) return 255;
+  return (uint32_t)(max((int)(top >> 23) - 127 - 2 + ((top & 0x7FFFFFu) > 0x600000u), -120) + 127);
+}
+__device__ __forceinline__ float micro_inverse(uint32_t byte) {  // 0 where the codes are 0 anyway
+  return byte == 0 || byte == 255 ? 0.f : __uint_as_float((254 - byte) << 23);
+}
+// Four values, and eight, already divided by their scale -> codes, nearest, ties to even, 6 at most.
+__device__ __forceinline__ uint32_t pack_four_bits(float a, float b, float c, float d) {
+  const uint32_t lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, a, b, 1.f, 0);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, c, d, 1.f, 1);
+}
+__device__ __forceinline__ uint32_t pack_eight_micro(const float (&x)[8], float inverse) {
+  if (inverse == 0.f) return 0u;
+  return pack_four_bits(x[0] * inverse, x[1] * inverse, x[2] * inverse, x[3] * inverse) |
+         pack_four_bits(x[4] * inverse, x[5] * inverse, x[6] * inverse, x[7] * inverse) << 16;
+}
+// Eight codes as the values that they stand for.
+__device__ __forceinline__ void unpack_micro(uint32_t w, uint32_t byte, float (&x)[8]) {
+  typedef float floatx2 __attribute__((ext_vector_type(2)));
+  const float scale = __uint_as_float(byte << 23);
+  const floatx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+  const floatx2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
 }
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {  // nearest, ties to even
@@ -203,6 +245,8 @@ struct AttendArgs {
 };
 AttendLayout attend_layout(const ams_params* p);
 hipError_t launch_attend(const AttendArgs& a, const AttendLayout& lay, bool bf16, int el, hipStream_t s);
+hipError_t launch_attend_e2m1(const AttendArgs& a, const AttendLayout& lay, bool bf16, hipStream_t s);
+void launch_attend_join(const AttendArgs& a, const AttendLayout& lay, bool bf16, hipStream_t s);
 
 struct RecodeArgs {
   Dims d;
@@ -223,6 +267,16 @@ struct EvictArgs {
   int32_t *idx, *n_kept, *lens_out;
   int budget, n_sink, n_last;
 };
+struct PagesArgs {
+  int batch, t_max, max_blocks, n_pages;
+  const int32_t *from, *to, *table;
+  int32_t *table_out, *ring;
+  const int32_t* state;
+  int32_t *state_out, *lens_out, *starts;
+  int64_t *slots, n_slots;
+};
+hipError_t launch_pages(const PagesArgs& a, hipStream_t s);
+
 size_t evict_ws_bytes(const ams_params* p);
 hipError_t launch_evict_pick(const EvictArgs& a, char* ws, hipStream_t s);
 

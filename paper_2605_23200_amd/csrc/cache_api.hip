@@ -1,4 +1,4 @@
-// Host side of the entry points around a bounded cache (ams_append, ams_attend, ams_recode, ams_evict): argument checks and the order
+// Host side of the entry points around a bounded cache (ams_append, ams_attend, ams_recode, ams_evict, ams_assign_pages): argument checks and the order
 // of the launches.  Nothing here touches device memory or waits for the stream.
 #include <math.h>
 
@@ -36,13 +36,15 @@ int check_evict(const ams_params* p) {
   return p->budget > (1 << 30) ? AMS_ERR_UNSUPPORTED : AMS_OK;
 }
 
-bool packed(const ams_cache* c) { return c->dtype == AMS_INT8 || c->dtype == AMS_E4M3; }
+bool micro(const ams_cache* c) { return c->dtype == AMS_E2M1; }
+bool packed(const ams_cache* c) { return c->dtype == AMS_INT8 || c->dtype == AMS_E4M3 || micro(c); }  // codes and scales
 
 // rows: positions per sequence that the call may touch.
 int check_cache(const ams_params* p, const ams_cache* c, int64_t rows) {
   if (!c || !c->kv.k || !c->kv.v || !aligned(c->kv.k) || !aligned(c->kv.v)) return AMS_ERR_INVALID_ARG;
   if (!packed(c) && c->dtype != p->kv_dtype) return AMS_ERR_INVALID_ARG;
   if (packed(c) && (!c->k_scale || !c->v_scale)) return AMS_ERR_INVALID_ARG;
+  if (micro(c) && (!aligned(c->k_scale) || !aligned(c->v_scale))) return AMS_ERR_INVALID_ARG;
   if (c->kv.layout == AMS_LAYOUT_DENSE) return c->kv.t_capacity < rows ? AMS_ERR_INVALID_ARG : AMS_OK;
   if (c->kv.layout != AMS_LAYOUT_PAGED) return AMS_ERR_INVALID_ARG;
   if (!c->kv.block_table || c->kv.max_blocks_per_seq < 1 || c->kv.n_slots < kBlockRows) return AMS_ERR_INVALID_ARG;
@@ -72,7 +74,7 @@ CacheDev device(const ams_params* p, const ams_cache* c, bool values) {
   r.n_slots = c->kv.n_slots;
   r.max_blocks = c->kv.max_blocks_per_seq;
   r.B = p->batch, r.H = p->n_kv_heads;
-  r.row_bytes = p->head_dim * (packed(c) ? 1 : c->dtype == AMS_BF16 ? 2 : 4);
+  r.row_bytes = micro(c) ? p->head_dim / 2 : p->head_dim * (packed(c) ? 1 : c->dtype == AMS_BF16 ? 2 : 4);
   r.paged = c->kv.layout == AMS_LAYOUT_PAGED;
   return r;
 }
@@ -209,6 +211,20 @@ int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens
   const CacheDev ks = device(p, src, false), vs = device(p, src, true), kd = device(p, dst, false), vd = device(p, dst, true);
   const RecodeArgs a{d, ks, vs, kd, vd, nullptr, idx, n_kept, p->budget, nullptr, nullptr, p->budget};
   return status(launch_recode(a, src->dtype, dst->dtype, s), s);
+}
+
+int ams_assign_pages(const ams_params* p, const ams_pages* x, const int32_t* lens_from, const int32_t* lens_to, int32_t* lens_out,
+                     int32_t* starts, int64_t* slots, int64_t n_slots, void* stream) {
+  const int rc = check_sizes(p);
+  if (rc) return rc;
+  if (!x || !x->table || !x->table_out || !x->ring || !x->state || !x->state_out || !lens_from || !lens_to) return AMS_ERR_INVALID_ARG;
+  if (x->max_blocks_per_seq < 1 || x->n_pages < 1 || n_slots < 0 || (n_slots > 0 && !slots)) return AMS_ERR_INVALID_ARG;
+  if ((int64_t)x->max_blocks_per_seq * kBlockRows < p->t_max) return AMS_ERR_INVALID_ARG;
+  if (x->state_out == x->state || lens_out == lens_from || lens_out == lens_to) return AMS_ERR_INVALID_ARG;
+  if ((int64_t)p->batch * p->t_max > INT32_MAX) return AMS_ERR_UNSUPPORTED;
+  const PagesArgs a{p->batch, p->t_max, x->max_blocks_per_seq, x->n_pages, lens_from, lens_to, x->table, x->table_out,
+                    x->ring, x->state, x->state_out, lens_out, starts, slots, n_slots};
+  return status(launch_pages(a, (hipStream_t)stream), (hipStream_t)stream);
 }
 
 }  // extern "C"
