@@ -130,7 +130,7 @@ void launch_join(const AttendArgs& a, const AttendLayout& lay, hipStream_t s) {
 
 }  // namespace
 
-AttendLayout attend_layout(const ams_params* p) {
+AttendLayout attend_layout(const ams_params* p, bool pairs) {
   AttendLayout r;
   const size_t units = (size_t)p->n_layers * p->batch * p->n_kv_heads, N = (size_t)p->group * p->window;
   const int tiles = div_up(N, 16);
@@ -145,7 +145,10 @@ AttendLayout attend_layout(const ams_params* p) {
   // paged units of up to 16384: 324 with 512, 329 with 1024, 349 with 2048, 412 with 4096; 4 units of 131072: 45.6 with 512, 44.7 in
   // one round, 48 in two; 256 ragged units of up to 16384 and 32 queries: 301, 281, 277, 282; 320 and 128 queries: 840, 730, 724, 781;
   // 64 units of 32768 and 32 queries: 201, 187, 178, 172 (the last is one round).
-  const size_t per_split = units * r.row_groups, resident = (r.row_tiles == 1 ? 3 : 2) - (p->kv_dtype == AMS_F32 && p->head_dim == 128);
+  // Pairs of heads (4 bits): two on a CU by their registers (one, two, three, four rounds of 256: 4 units of 131072 26, 27, 31, 33 us; 32
+  // ragged units of up to 16384 22.4, 22.1, 24.5, 24.3; 128 of up to 8192 35, 34, 31, 35; 512 of 2176 48, 51, 53, 50).
+  r.pairs = pairs;
+  const size_t per_split = units * r.row_groups / (pairs ? 2 : 1), resident = pairs ? 2 : (r.row_tiles == 1 ? 3 : 2) - (p->kv_dtype == AMS_F32 && p->head_dim == 128);
   const int fine = r.row_tiles == 1 ? 512 : 2048;
   if (per_split * div_up(p->t_max, fine) >= 2048) {
     r.chunk = fine;

@@ -279,6 +279,16 @@ struct KTile {
   __device__ __forceinline__ float of_logits() const { return kMicro<EL> ? 1.f : scale; }
 };
 
+// Scale bytes of two times four positions as powers of two.
+__device__ __forceinline__ void four_powers(const uint32_t (&scales)[2], float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t b = scales[j >> 2];
+    const int up = 23 - 8 * (j & 3);
+    x[j] = __uint_as_float((up >= 0 ? b << up : b >> -up) & 0x7F800000u);
+  }
+}
+
 // Two blocks of V: lane % 16 is the stretch of HD / 16 channels, word [j] of position 4 (lane / 16) + j % 4 of block j / 4.
 template <int EL, int HD>
 struct VTile {
@@ -312,16 +322,34 @@ struct VTile {
       }
     }
   }
-  // In 4 bits: the scales as powers of two, by position.
-  __device__ __forceinline__ void powers(float (&x)[8]) const {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t b = scales[j >> 2];
-      const int up = 23 - 8 * (j & 3);
-      x[j] = __uint_as_float((up >= 0 ? b << up : b >> -up) & 0x7F800000u);
-    }
-  }
 };
+
+// Channels d0 .. d0 + HD / 16 - 1 of a query's sums over a split: the output where there is one split, else for the join.
+template <bool BF16, int HD>
+__device__ __forceinline__ void finish_query(const AttendArgs& a, int unit, int n, int split, float top, float all, const float (&x)[HD / 16], int d0) {
+  const int N = a.d.N;
+  const bool last = a.n_splits == 1;
+  const int64_t row = ((int64_t)unit * a.n_splits + split) * N + n;
+  if (threadIdx.x % 16 == 0) {
+    a.stats[((int64_t)unit * N + n) * a.n_splits + split] = make_float2(top, all);
+    if (last && a.lse) a.lse[(int64_t)unit * N + n] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
+  }
+  if (last) {
+    const float inverse = all == 0.f ? 0.f : 1.f / all;
+    char* to = a.out + (((int64_t)unit * N + n) * HD + d0) * (BF16 ? 2 : 4);
+#pragma unroll
+    for (int e = 0; e < HD / 16; e += 4) {
+      const float y0 = x[e] * inverse, y1 = x[e + 1] * inverse, y2 = x[e + 2] * inverse, y3 = x[e + 3] * inverse;
+      if constexpr (BF16)
+        *(uint2*)(to + 2 * e) = make_uint2(bf16_pair(y0, y1), bf16_pair(y2, y3));
+      else
+        *(float4*)(to + 4 * e) = make_float4(y0, y1, y2, y3);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < HD / 16; e += 4) *(float4*)&a.part[row * HD + d0 + e] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+  }
+}
 
 // One split of one unit's positions for 16 R row_waves of its queries: row_waves waves side by side take 16 R queries each, the others
 // every (4 / row_waves)-th step of the positions.
@@ -449,7 +477,7 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
     float vscale[2], vpower[8];
     if constexpr (kMicro<EL>) {
       if constexpr (!MORE) vt.scales[0] &= off.v_there[0], vt.scales[1] &= off.v_there[1];  // (the sequence's end lies in a last step)
-      vt.powers(vpower);
+      four_powers(vt.scales, vpower);
       uint32_t most = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(vpower[j]));
@@ -548,7 +576,6 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
     step(std::false_type{});
   }
   // the waves of the same queries together: 16 queries at a time, thread (query, stretch of HD / 16 channels)
-  const bool last = a.n_splits == 1;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (r > 0) __syncthreads();
@@ -575,26 +602,7 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
 #pragma unroll
         for (int e = 0; e < TILES; ++e) x[e] = fmaf(f, joint[w][qr][d0 + e], x[e]);
       }
-      const int64_t row = ((int64_t)unit * a.n_splits + split) * N + n;
-      if (threadIdx.x % 16 == 0) {
-        a.stats[((int64_t)unit * N + n) * a.n_splits + split] = make_float2(top, all);
-        if (last && a.lse) a.lse[(int64_t)unit * N + n] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
-      }
-      if (last) {
-        const float inverse = all == 0.f ? 0.f : 1.f / all;
-        char* to = a.out + (((int64_t)unit * N + n) * HD + d0) * (BF16 ? 2 : 4);
-#pragma unroll
-        for (int e = 0; e < TILES; e += 4) {
-          const float y0 = x[e] * inverse, y1 = x[e + 1] * inverse, y2 = x[e + 2] * inverse, y3 = x[e + 3] * inverse;
-          if constexpr (BF16)
-            *(uint2*)(to + 2 * e) = make_uint2(bf16_pair(y0, y1), bf16_pair(y2, y3));
-          else
-            *(float4*)(to + 4 * e) = make_float4(y0, y1, y2, y3);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < TILES; e += 4) *(float4*)&a.part[row * HD + d0 + e] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-      }
+      finish_query<BF16, HD>(a, unit, n, split, top, all, x, d0);
     }
   }
 }

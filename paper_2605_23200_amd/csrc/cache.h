@@ -210,6 +210,7 @@ struct AttendLayout {
   size_t part, stats, joined, stash, total;  // outputs and statistics of the splits, logits
   int chunk, n_splits, row_tiles, row_waves, row_groups;
   bool stashed;  // the logits are kept for the weights
+  bool pairs;    // of heads (4 bits)
 };
 
 // ---- launchers ----
@@ -243,7 +244,7 @@ struct AttendArgs {
   float* stash;   // [units, blocks, N, 16]
   int chunk, n_splits, row_waves;
 };
-AttendLayout attend_layout(const ams_params* p);
+AttendLayout attend_layout(const ams_params* p, bool pairs);
 hipError_t launch_attend(const AttendArgs& a, const AttendLayout& lay, bool bf16, int el, hipStream_t s);
 hipError_t launch_attend_e2m1(const AttendArgs& a, const AttendLayout& lay, bool bf16, hipStream_t s);
 void launch_attend_join(const AttendArgs& a, const AttendLayout& lay, bool bf16, hipStream_t s);
