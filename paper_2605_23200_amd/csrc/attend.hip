@@ -94,31 +94,42 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a, int
   }
   const int first = turned_x(joins) * kStashKeys;
   if (first >= T) return;
+  // The first logits and the weights are on their way while the statistics are joined.
+  constexpr int AHEAD = 4;
+  const int t = first + 4 * threadIdx.x;
+  const float* x = a.stash + (((int64_t)unit * ((a.d.t_max + 15) / 16) + min(t, T - 1) / 16) * N) * 16 + t % 16;
+  const int64_t at = (int64_t)unit * a.d.t_stride + t;
+  float4 ahead[AHEAD];
+  float w[4];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) ahead[i] = *(const float4*)(x + min(i, N - 1) * 16);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = a.weights_in && t + i < T ? a.weights_in[at + i] : 0.f;
   {
     const int n = threadIdx.x >> 4;
     const float2 st = joined_stats<16>(a, unit, min(n, N - 1), splits, threadIdx.x & 15);
     if ((threadIdx.x & 15) == 0) stat[n] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
   }
   __syncthreads();
-  const int t = first + 4 * threadIdx.x;
   if (t >= T) return;
-  const float* x = a.stash + (((int64_t)unit * ((a.d.t_max + 15) / 16) + t / 16) * N) * 16 + t % 16;
-  float w[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int n = 0; n < N; ++n) {
-    const float4 v = *(const float4*)(x + n * 16);
+  float more[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](const float4& v, int n) __attribute__((always_inline)) {
     const float s[4] = {v.x, v.y, v.z, v.w};
     const float2 st = stat[n];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {  // (a position that the query does not see has no part in a sum that is no number)
       const float p = power_of_two(s[i] - st.x) * st.y;
-      w[i] += s[i] == -INFINITY ? 0.f : p;
+      more[i] += s[i] == -INFINITY ? 0.f : p;
     }
-  }
-  const int64_t at = (int64_t)unit * a.d.t_stride + t;
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < N) add(ahead[i], i);
+#pragma unroll 4
+  for (int n = AHEAD; n < N; ++n) add(*(const float4*)(x + n * 16), n);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (t + i < T) a.weights_out[at + i] = (a.weights_in ? a.weights_in[at + i] : 0.f) + w[i];
+    if (t + i < T) a.weights_out[at + i] = w[i] + more[i];
 }
 
 template <bool BF16, int HD>

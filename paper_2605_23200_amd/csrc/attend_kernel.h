@@ -438,12 +438,13 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
       kt[1].load(u, slot[1], off.k[1], off.k_scale[1]);
       find(next + stride);
     }
-    float x[R][8];
+    float x[R][8];  // logits in units of log2; in 4 bits with several tiles still without that factor, which is the same for all
+    constexpr bool RAW = kMicro<EL> && R > 1;
     bool higher = false;
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[r][j] = s[j >> 2][r][j & 3] * kscale[j >> 2];
+      for (int j = 0; j < 8; ++j) x[r][j] = RAW ? s[j >> 2][r][j & 3] : s[j >> 2][r][j & 3] * kscale[j >> 2];
     if (!whole) {
 #pragma unroll
       for (int r = 0; r < R; ++r)
@@ -457,6 +458,7 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
       top[r] = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 8; ++j) top[r] = fmaxf(top[r], x[r][j]);
+      if constexpr (RAW) top[r] *= to_log2;
       higher = higher || top[r] > m[r] + kSlack;
     }
     if (__any(higher)) {
@@ -525,7 +527,11 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
       uint32_t t[3][4];
 #pragma unroll
       for (int j = 0; j < 8; j += 2) {
-        float p0 = power_of_two(x[r][j] - m[r]), p1 = power_of_two(x[r][j + 1] - m[r]);
+        float p0, p1;
+        if constexpr (RAW)
+          p0 = power_of_two(fmaf(x[r][j], to_log2, -m[r])), p1 = power_of_two(fmaf(x[r][j + 1], to_log2, -m[r]));
+        else
+          p0 = power_of_two(x[r][j] - m[r]), p1 = power_of_two(x[r][j + 1] - m[r]);
         sum[r] += p0 + p1;
         if constexpr (!kMicro<EL>) p0 *= vscale[j >> 2], p1 *= vscale[j >> 2];
 #pragma unroll
