@@ -5,8 +5,10 @@
 // workgroup forms for itself (batch * 8 bytes out of the cache; a second launch that waited for the first's sums would cost more
 // than they do).  Pages are taken from the front of the free stretch as it was before the call and put behind its end, so that no
 // workgroup reads what another writes: the stretches cannot meet, since a page is free or with a sequence.
-// What bounds it: latency (lengths, sums over a workgroup, search, page, slot follow from one another), then the bytes of the tables
-// and slots.
+// What bounds it: latency (launch, lengths, sums over a workgroup: 3.6 of 4.2 us for 64 sequences with a token each), then the
+// instructions that a stretch of a table and a slot take: 768 sequences of up to 32768 positions and 750000 slots, 19 MB, in 11.3 us, of
+// which 4.5 are the sums.  (A wave that writes the slots of its stretch of a table from the pages that it has found, without a search:
+// 13 us, since the tokens of a prompt are with few waves; 256 slots a wave at a time: 12.5.)
 #include "cache.h"
 
 namespace ams {
@@ -14,7 +16,8 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kHeld = 2048;    // sequences whose lengths lie in LDS
-constexpr int kStretch = 256;  // entries of a table, and slots, a wave takes at a time
+constexpr int kStretch = 128;  // entries of a table that a wave takes at a time
+constexpr int kSlots = 64;     // slots, likewise
 
 struct Lens {
   int from, to;
@@ -58,12 +61,21 @@ __global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a) {
   auto lens = [&](int b) __attribute__((always_inline)) { return held ? Lens{from_held[b], to_held[b]} : read(b); };
   const int count = min(max(a.state[1], 0), a.n_pages), given_head = a.state[0];
   const int head = given_head < 0 || given_head >= a.n_pages ? 0 : given_head;
+  if (held) {
+    Lens x[kHeld / kThreads];  // (all loads at once)
+#pragma unroll
+    for (int i = 0; i < kHeld / kThreads; ++i)
+      if (i * kThreads < a.batch) x[i] = read(min(i * kThreads + (int)threadIdx.x, a.batch - 1));
+#pragma unroll
+    for (int i = 0; i < kHeld / kThreads; ++i)
+      if (i * kThreads < a.batch) from_held[i * kThreads + threadIdx.x] = x[i].from, to_held[i * kThreads + threadIdx.x] = x[i].to;
+    __syncthreads();
+  }
   // a thread's stretch of sequences
   const int per = (a.batch + kThreads - 1) / kThreads, b0 = min((int)threadIdx.x * per, a.batch), b1 = min(b0 + per, a.batch);
   int asked = 0, freed = 0, fresh = 0;
   for (int b = b0; b < b1; ++b) {
-    const Lens x = read(b);
-    if (held) from_held[b] = x.from, to_held[b] = x.to;
+    const Lens x = lens(b);
     asked += x.asked(), freed += x.freed(), fresh += x.fresh();
   }
   int all_asked, all_freed, all_fresh;
@@ -97,8 +109,8 @@ __global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a) {
     const int64_t at = head + i;
     return a.ring[at >= a.n_pages ? at - a.n_pages : at];
   };
-  const int64_t pieces = (a.max_blocks + kStretch - 1) / kStretch, tables = pieces * a.batch, slots = (a.n_slots + kStretch - 1) / kStretch;
-  for (int64_t task = blockIdx.x * kWaves + wave; task < tables + slots; task += gridDim.x * kWaves) {
+  const uint32_t pieces = (a.max_blocks + kStretch - 1) / kStretch, tables = pieces * a.batch, tasks = tables + (uint32_t)((a.n_slots + kSlots - 1) / kSlots);
+  for (uint32_t task = blockIdx.x * kWaves + wave; task < tasks; task += gridDim.x * kWaves) {
     if (task < tables) {  // a stretch of one sequence's row
       const int b = (int)(task / pieces), first = (int)(task % pieces) * kStretch;
       int asked_at = asked_before[b / per], freed_at = freed_before[b / per];
@@ -108,26 +120,45 @@ __global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a) {
       }
       const Lens x = lens(b);
       const bool served = x.asked() == 0 || asked_at + x.asked() <= count;
-      const int had = x.had(), want = served ? x.want() : had, stay = min(had, want);
-      const int64_t row = (int64_t)b * a.max_blocks;
+      const int had = x.had(), want = served ? x.want() : had, stay = min(had, want), behind = max(had, want);
+      const int32_t* row = a.table + (int64_t)b * a.max_blocks;
+      int32_t* to = a.table_out + (int64_t)b * a.max_blocks;
+      if (first + kStretch <= stay) {  // pages that stay
+        if (to == row) continue;
+        int page[kStretch / 64];
+#pragma unroll
+        for (int k = 0; k < kStretch / 64; ++k) page[k] = row[first + 64 * k + lane];
+#pragma unroll
+        for (int k = 0; k < kStretch / 64; ++k) to[first + 64 * k + lane] = page[k];
+        continue;
+      }
+      const int last = min(first + kStretch, a.max_blocks);
+      if (first >= behind) {  // none
+        for (int j = first + lane; j < last; j += 64) to[j] = -1;
+        continue;
+      }
 #pragma unroll
       for (int k = 0; k < kStretch; k += 64) {
         const int j = first + k + lane;
-        if (j >= a.max_blocks) continue;
+        if (j >= last) continue;
         int page = -1;
-        if (j < had) page = a.table[row + j];
+        if (j < had) page = row[j];
         if (j >= want && j < had) {
           a.ring[((int64_t)head + count + freed_at + j - want) % a.n_pages] = page;
           page = -1;
         }
         if (j >= had && j < want) page = taken((int64_t)asked_at + j - had);
-        if (j >= stay || a.table_out != a.table) a.table_out[row + j] = page;
+        if (j >= stay || to != row) to[j] = page;
       }
       continue;
     }
-    const int64_t first = (task - tables) * kStretch;
+    const int64_t first = (int64_t)(task - tables) * kSlots;
+    if (first >= all_fresh) {  // behind the last token
+      for (int64_t i = first + lane; i < min(first + kSlots, a.n_slots); i += 64) a.slots[i] = -1;
+      continue;
+    }
 #pragma unroll
-    for (int k = 0; k < kStretch; k += 64) {
+    for (int k = 0; k < kSlots; k += 64) {
       const int64_t i = first + k + lane;
       if (i >= a.n_slots) continue;
       int64_t slot = -1;
@@ -156,11 +187,13 @@ __global__ __launch_bounds__(kThreads) void pages_kernel(PagesArgs a) {
 }  // namespace
 
 hipError_t launch_pages(const PagesArgs& a, hipStream_t s) {
-  const int64_t tasks = (int64_t)div_up(a.max_blocks, kStretch) * a.batch + (a.n_slots + kStretch - 1) / kStretch;
-  // (workgroups that read a long batch's lengths to little end would read more of them than there is to write)
-  const int64_t most = a.batch <= kHeld ? 2048 : 256;
+  const int64_t tasks = (int64_t)div_up(a.max_blocks, kStretch) * a.batch + (a.n_slots + kSlots - 1) / kSlots;
+  if (tasks > INT32_MAX) return hipErrorNotSupported;
+  // Six workgroups on a CU: more of them form the sums more often than their waves gain (768 sequences: 12.2 us with three, 11.7 with four,
+  // 11.3 with six, 12.8 with eight); where the lengths of a long batch are read anew by each, one.
+  const int64_t most = a.batch <= kHeld ? 1536 : 256;
   prof_mark("pages", s);
-  hipLaunchKernelGGL(pages_kernel, dim3((unsigned)max((int64_t)1, min((tasks + kWaves - 1) / kWaves, most))), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(pages_kernel, dim3((unsigned)min((tasks + kWaves - 1) / kWaves, most)), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
