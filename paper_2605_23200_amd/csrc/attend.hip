@@ -156,10 +156,11 @@ AttendLayout attend_layout(const ams_params* p, bool pairs) {
   // paged units of up to 16384: 324 with 512, 329 with 1024, 349 with 2048, 412 with 4096; 4 units of 131072: 45.6 with 512, 44.7 in
   // one round, 48 in two; 256 ragged units of up to 16384 and 32 queries: 301, 281, 277, 282; 320 and 128 queries: 840, 730, 724, 781;
   // 64 units of 32768 and 32 queries: 201, 187, 178, 172 (the last is one round).
-  // Pairs of heads (4 bits): two on a CU by their registers (one, two, three, four rounds of 256: 4 units of 131072 26, 27, 31, 33 us; 32
-  // ragged units of up to 16384 22.4, 22.1, 24.5, 24.3; 128 of up to 8192 35, 34, 31, 35; 512 of 2176 48, 51, 53, 50).
+  // Pairs of heads (4 bits): one on a CU, with twice the loads in flight (one, two, three, four on a CU: 4 units of 131072 26, 27, 31, 33 us;
+  // 32 units of 16384 23.3, 24.2, 25.9, 27.0, ragged ones 22.4, 22.1, 24.5, 24.3; 128 of 8192 45, 48, 51, 49, ragged ones 35, 34, 31, 35).  That
+  // is never more splits than head by head, so the workspace for any cache is that of one head at a time.
   r.pairs = pairs;
-  const size_t per_split = units * r.row_groups / (pairs ? 2 : 1), resident = pairs ? 2 : (r.row_tiles == 1 ? 3 : 2) - (p->kv_dtype == AMS_F32 && p->head_dim == 128);
+  const size_t per_split = units * r.row_groups / (pairs ? 2 : 1), resident = pairs ? 1 : (r.row_tiles == 1 ? 3 : 2) - (p->kv_dtype == AMS_F32 && p->head_dim == 128);
   const int fine = r.row_tiles == 1 ? 512 : 2048;
   if (per_split * div_up(p->t_max, fine) >= 2048) {
     r.chunk = fine;

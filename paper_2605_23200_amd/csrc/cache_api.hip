@@ -157,11 +157,7 @@ int ams_append(const ams_params* p, const ams_new_tokens* x, const ams_rope* rop
   return status(launch_append(a, rope, p->kv_dtype == AMS_BF16, dst->dtype, (hipStream_t)stream), (hipStream_t)stream);
 }
 
-size_t ams_attend_workspace_bytes(const ams_params* p) {  // for any cache that the parameters fit
-  if (check_attend(p) != AMS_OK) return 0;
-  const size_t one = attend_layout(p, false).total, two = p->n_kv_heads % 2 ? 0 : attend_layout(p, true).total;
-  return one > two ? one : two;
-}
+size_t ams_attend_workspace_bytes(const ams_params* p) { return check_attend(p) == AMS_OK ? attend_layout(p, false).total : 0; }
 size_t ams_evict_workspace_bytes(const ams_params* p) { return check_evict(p) == AMS_OK ? evict_ws_bytes(p) : 0; }
 
 int ams_attend(const ams_params* p, const ams_cache* src, const int32_t* seq_lens, const void* q, void* out, float* lse,
