@@ -92,12 +92,14 @@ _lib = None
 
 
 def lib() -> C.CDLL:
-    """Loads the built library; raises if it has not been built (no fallback exists)."""
-    global _lib
+    """Loads the built library and the checks of tensor arguments; raises if they have not been built (no fallback exists)."""
+    global _lib, _arg, _token_rows
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: run `python -m paper_2605_23200_amd.build` "
                               "(or __graft_entry__.build()) first")
+        from . import _args
+        _arg, _token_rows = _args.arg, _args.token_rows
         l = C.CDLL(LIB_PATH)
         l.ams_status_string.restype = C.c_char_p
         l.ams_status_string.argtypes = [C.c_int]
@@ -309,12 +311,15 @@ def _cache_for(p: Params, c: Cache):
 
 
 def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, gpu: int, what: str):
-    """Pointer of a contiguous tensor of at least `numel` elements on that GPU; None stays None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.get_device() != gpu or t.numel() < numel or not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous {dtype} tensor of at least {numel} elements on GPU {gpu} expected")
-    return t.data_ptr()
+    """Pointer of a contiguous tensor of at least `numel` elements on that GPU; None stays None.  (Compiled, csrc/args.cpp: lib() puts it here.)"""
+    lib()
+    return _arg(t, dtype, numel, gpu, what)
+
+
+def _token_rows(t: torch.Tensor, shape, dtype: torch.dtype, gpu: int, what: str):
+    """(pointer, elements from token to token) of [L, B, n_new, heads, D]: any slice of a projection's output along the heads.  (Compiled as well.)"""
+    lib()
+    return _token_rows(t, shape, dtype, gpu, what)
 
 
 def _launch(fn, what: str, gpu: int, stream, *args):
@@ -331,19 +336,6 @@ def _launch(fn, what: str, gpu: int, stream, *args):
 
 
 _ROWS = {F32: torch.float32, BF16: torch.bfloat16}
-
-
-def _token_rows(t: torch.Tensor, shape, dtype, gpu: int, what: str):
-    """(pointer, elements from token to token) of [L, B, n_new, heads, D]: any slice of a projection's output along the heads."""
-    L, batch, n_new, heads, D = shape
-    s0, s1, s2, s3, s4 = t.stride() if t.dim() == 5 else (0,) * 5
-    if t.dtype is not dtype or t.get_device() != gpu or t.shape != shape or s4 != 1 or (heads > 1 and s3 != D):
-        raise ValueError(f"{what}: {dtype} {list(shape)} (layers, batch, new, heads, channels) on GPU {gpu} with contiguous heads expected")
-    # one stride from token to token, over those of a sequence, the batch and the layers (extents of one have none)
-    step = s2 if n_new > 1 else s1 if batch > 1 else s0 if L > 1 else heads * D
-    if (batch > 1 and s1 != step * n_new) or (L > 1 and s0 != step * n_new * batch):
-        raise ValueError(f"{what}: one stride from token to token expected")
-    return t.data_ptr(), step
 
 
 def ams_append(p, q, k, v, q_weight, k_weight, norm_eps, rope, positions, seq_lens, q_out, dst, lens_out=None, stream=None):
@@ -368,13 +360,13 @@ def ams_attend_workspace_bytes(p: Params) -> int:
 
 
 def ams_attend(p, src, seq_lens, q, out, ws, lse=None, weights_in=None, weights_out=None, stream=None):
-    gpu, rows = _cache_for(p, src), _ROWS[p.kv_dtype]
-    n = p.units * p.group * p.window
+    gpu, rows, batch, D = _cache_for(p, src), _ROWS[p.kv_dtype], p.batch, p.head_dim
+    units = p.n_layers * batch * p.n_kv_heads
+    n, weights = units * p.group * p.window, units * p.t_stride
     _launch((_lib or lib()).ams_attend, "ams_attend", gpu, stream, C.byref(p), C.byref(src),
-            _arg(seq_lens, torch.int32, p.batch, gpu, "seq_lens"), _arg(q, rows, n * p.head_dim, gpu, "q"),
-            _arg(out, rows, n * p.head_dim, gpu, "out"), _arg(lse, torch.float32, n, gpu, "lse"),
-            _arg(weights_in, torch.float32, p.units * p.t_stride, gpu, "weights_in"),
-            _arg(weights_out, torch.float32, p.units * p.t_stride, gpu, "weights_out"),
+            _arg(seq_lens, torch.int32, batch, gpu, "seq_lens"), _arg(q, rows, n * D, gpu, "q"),
+            _arg(out, rows, n * D, gpu, "out"), _arg(lse, torch.float32, n, gpu, "lse"),
+            _arg(weights_in, torch.float32, weights, gpu, "weights_in"), _arg(weights_out, torch.float32, weights, gpu, "weights_out"),
             _arg(ws, torch.uint8, 0, gpu, "ws"), ws.numel())
 
 
@@ -382,11 +374,13 @@ def ams_recode(p, src, seq_lens, dst, idx=None, n_kept=None, credit_src=None, cr
     gpu = _cache_for(p, src)
     if _cache_for(p, dst) != gpu:
         raise ValueError("both caches lie on one GPU")
+    units = p.units
+    kept = units * p.budget
     _launch((_lib or lib()).ams_recode, "ams_recode", gpu, stream, C.byref(p), C.byref(src),
-            _arg(seq_lens, torch.int32, p.batch, gpu, "seq_lens"), _arg(idx, torch.int32, p.units * p.budget, gpu, "idx"),
-            _arg(n_kept, torch.int32, p.units, gpu, "n_kept"), C.byref(dst),
-            _arg(credit_src, torch.float32, p.units * p.t_stride, gpu, "credit_src"),
-            _arg(credit_dst, torch.float32, p.units * p.budget, gpu, "credit_dst"))
+            _arg(seq_lens, torch.int32, p.batch, gpu, "seq_lens"), _arg(idx, torch.int32, kept, gpu, "idx"),
+            _arg(n_kept, torch.int32, units, gpu, "n_kept"), C.byref(dst),
+            _arg(credit_src, torch.float32, units * p.t_stride, gpu, "credit_src") if credit_src is not None else None,
+            _arg(credit_dst, torch.float32, kept, gpu, "credit_dst"))
 
 
 def ams_evict_workspace_bytes(p: Params) -> int:
