@@ -342,17 +342,27 @@ def test_append_no_number_and_infinite():
 
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
 @pytest.mark.parametrize("group,W,causal,paged", [(1, 1, False, False), (4, 1, True, True), (2, 8, True, False), (5, 5, False, True),
-                                                 (8, 8, True, False), (7, 11, True, True), (8, 32, True, False)])
+                                                 (8, 8, True, False), (7, 11, True, True), (8, 32, True, False), (2, 4, True, True),
+                                                 (1, 8, True, False), (7, 1, False, True), (3, 2, True, False)])
 def test_attend_shapes(dtype, D, group, W, causal, paged):
-    """Every row tile, the two ways to the weights; lengths at the edges of blocks, steps and chunks, shorter than the window, empty."""
+    """Every row tile, heads two at a time (up to 8 queries), the two ways to the weights; lengths at the edges of blocks, steps and chunks,
+    shorter than the window, empty."""
     lens = [0, 1, 15, 16, 17, 31, 33, 127, 128, 130, 257, 700]
     _attend_case(filled((1, len(lens), 2, D), 701, lens, paged, 5), lens, group, W, dtype, causal, "new", t_stride=705)
 
 
-@pytest.mark.parametrize("T", [1, 511, 4100, 20003])
+@pytest.mark.parametrize("heads", [1, 3, 4])
+@pytest.mark.parametrize("group,W", [(4, 1), (2, 4), (3, 5)])
+def test_attend_heads_odd_and_even(heads, group, W):
+    lens = [300, 77, 0]
+    for paged in (False, True):
+        _attend_case(filled((2, 3, heads, 128), 305, lens, paged, 15), lens, group, W, causal=True)
+
+
+@pytest.mark.parametrize("T,heads", [(1, 1), (1, 2), (511, 1), (511, 2), (4100, 1), (4100, 2), (20003, 1), (9001, 2)])
 @pytest.mark.parametrize("group,W", [(4, 1), (7, 1), (4, 9)])
-def test_attend_lengths_of_one_unit(T, group, W):
-    _attend_case(filled((1, 1, 1, 128), T + 5, [T], False, 6), [T], group, W, causal=True)
+def test_attend_lengths_of_one_sequence(T, heads, group, W):
+    _attend_case(filled((1, 1, heads, 128), T + 5, [T], False, 6), [T], group, W, causal=True)
 
 
 @pytest.mark.parametrize("weights,lse", [("new", False), ("same", True), ("zero", True), (None, True), (None, False)])
@@ -366,10 +376,12 @@ def test_attend_lengths_outside_the_cache_are_clamped():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_attend_extreme_scales_and_logits(dtype):
-    """Logits of thousands (one position takes all), rows of V 2^60 apart, channels of V 2^50 apart, rows of zeros, an all-zero cache."""
+@pytest.mark.parametrize("heads", [1, 2])
+def test_attend_extreme_scales_and_logits(dtype, heads):
+    """Logits of thousands (one position takes all), rows of V 2^60 apart, channels of V 2^50 apart, rows of zeros, an all-zero cache; beside
+    an ordinary head."""
     lens = [400] * 4
-    cache = filled((1, 4, 1, 128), 400, lens, False, 9)
+    cache = filled((1, 4, heads, 128), 400, lens, False, 9)
     rng = np.random.default_rng(2)
     cache.fill("k", 0, 0, 0, loud_rows(rng, 400, 128) * 300)
     v = loud_rows(rng, 400, 128)
@@ -383,7 +395,7 @@ def test_attend_extreme_scales_and_logits(dtype):
     cache.fill("v", 0, 2, 0, v)
     cache.fill("k", 0, 3, 0, np.zeros((400, 128)))
     cache.fill("v", 0, 3, 0, np.zeros((400, 128)))
-    for W, causal in ((1, False), (12, True)):
+    for W, causal in ((1, False), (2, True), (12, True)):
         _attend_case(cache, lens, 3, W, dtype, causal)
 
 
@@ -423,29 +435,30 @@ def test_attend_through_a_bad_table_entry_stays_in_the_pool():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("group,W", [(2, 4), (1, 16), (2, 24), (3, 40)])
-def test_attend_nan_scales(D, group, W, dtype):
+@pytest.mark.parametrize("heads", [3, 4])
+@pytest.mark.parametrize("group,W", [(2, 4), (1, 8), (1, 16), (2, 24), (3, 40)])
+def test_attend_nan_scales(heads, D, group, W, dtype):
     """32 channels of a key that are no number make the outputs of the queries that see its position NaN; of a value, those 32 outputs of those
     queries; not other queries, heads, channels; not through positions behind the last one, whose bytes may be anything."""
     lens = [160, 147]
-    cache = filled((1, 2, 3, D), 200, lens, False, 4)
+    cache = filled((1, 2, heads, D), 200, lens, False, 4)
     bad = {}
     for b, T in enumerate(lens):
-        for h, (name, back, part) in enumerate((("k", 3, 0), ("v", 2, D // GROUP - 1), ("v", 7 * 2, 0))):
+        for h, (name, back, part) in enumerate((("k", 3, 0), ("v", 2, D // GROUP - 1), ("v", 7 * 2, 0), ("k", 12, D // GROUP - 1))[:heads]):
             t = T - back
             codes, byte = cache.get(name, 0, b, h, t)
             byte[part] = 255
             codes[part * GROUP:(part + 1) * GROUP] = 0
             cache.put(name, 0, b, h, t, codes, byte)
             bad[b, h] = (name, t, part)
-        for h in range(3):                              # behind the last one: every scale no number
+        for h in range(heads):                          # behind the last one: every scale no number
             for t in range(T, blocks(T) * BLOCK):
                 for name in ("k", "v"):
                     cache.put(name, 0, b, h, t, np.full(D, 7), np.full(D // GROUP, 255))
-    p = params((1, 2, 3, D), 200, group=group, window=W, causal=True, dtype=dtype)
-    q = torch.randn((1, 2, 3 * group, W, D)).to(ROWS[dtype])
+    p = params((1, 2, heads, D), 200, group=group, window=W, causal=True, dtype=dtype)
+    q = torch.randn((1, 2, heads * group, W, D)).to(ROWS[dtype])
     out = torch.zeros_like(q, device=DEV)
-    w = torch.zeros((6, 200), device=DEV)
+    w = torch.zeros((2 * heads, 200), device=DEV)
     ws = torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
     B.ams_attend(p, cache.upload(), lens_dev(lens), q.to(DEV), out, ws, None, None, w)
     nan = torch.isnan(out.float()).cpu()[0]             # [batch, heads * group, W, D]
@@ -456,26 +469,31 @@ def test_attend_nan_scales(D, group, W, dtype):
         for g in range(group):
             assert torch.equal(nan[b, h * group + g], want), (b, h, g)
         if name == "v":
-            assert not torch.isnan(w[b * 3 + h]).any()
-    _attend_case(filled((1, 2, 3, D), 200, lens, False, 4), lens, group, W, dtype, True)     # the same caches without them
+            assert not torch.isnan(w[b * heads + h]).any()
 
 
-@pytest.mark.parametrize("W", [4, 24])
-def test_attend_a_query_that_is_no_number(W):
+@pytest.mark.parametrize("heads", [1, 2])
+@pytest.mark.parametrize("W", [3, 4, 24])
+def test_attend_a_query_that_is_no_number(heads, W):
+    """The first query of one head's window: its output, its lse and the weights of what it sees; not those of the positions behind it, and
+    nothing of the other head."""
     T = 160
-    cache = filled((1, 1, 1, 64), 200, [T], False, 4)
-    p = params((1, 1, 1, 64), 200, group=2, window=W, causal=True)
-    q = torch.randn((1, 1, 2, W, 64)).to(torch.bfloat16)
-    q[0, 0, 1, 0] = math.nan
-    out, lse = torch.zeros_like(q, device=DEV), torch.zeros((1, 1, 2, W), device=DEV)
-    w = torch.zeros((1, 200), device=DEV)
-    ws = torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
-    B.ams_attend(p, cache.upload(), lens_dev([T]), q.to(DEV), out, ws, lse, None, w)
-    bad = torch.zeros((2, W), dtype=torch.bool)
-    bad[1, 0] = True
-    assert torch.equal(torch.isnan(out.float()).all(-1).cpu()[0, 0], bad) and torch.equal(torch.isnan(out.float()).any(-1).cpu()[0, 0], bad)
-    assert torch.equal(torch.isnan(lse).cpu()[0, 0], bad)
-    assert torch.equal(torch.isnan(w[0, :T]).cpu(), torch.arange(T) < T - W + 1)
+    cache = filled((1, 1, heads, 64), 200, [T], False, 4)
+    p = params((1, 1, heads, 64), 200, group=2, window=W, causal=True)
+    q = torch.randn((1, 1, 2 * heads, W, 64)).to(torch.bfloat16)
+    for h in range(heads):
+        x = q.clone()
+        x[0, 0, 2 * h + 1, 0] = math.nan
+        out, lse = torch.zeros_like(q, device=DEV), torch.zeros((1, 1, 2 * heads, W), device=DEV)
+        w = torch.zeros((heads, 200), device=DEV)
+        ws = torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+        B.ams_attend(p, cache.upload(), lens_dev([T]), x.to(DEV), out, ws, lse, None, w)
+        bad = torch.zeros((2 * heads, W), dtype=torch.bool)
+        bad[2 * h + 1, 0] = True
+        assert torch.equal(torch.isnan(out.float()).all(-1).cpu()[0, 0], bad) and torch.equal(torch.isnan(out.float()).any(-1).cpu()[0, 0], bad)
+        assert torch.equal(torch.isnan(lse).cpu()[0, 0], bad)
+        for g in range(heads):
+            assert torch.equal(torch.isnan(w[g, :T]).cpu(), torch.arange(T) < (T - W + 1 if g == h else 0))
 
 
 def test_attend_two_calls_give_the_same_bits():
@@ -516,6 +534,33 @@ def test_pools_beyond_32_bits():
         outs.append((out, w, back.dev["k"], back.dev["v"]))
     for x, y in zip(*outs):
         same_bits(x, y)
+
+
+def test_slabs_of_very_many_rows():
+    """Slabs so long that the way from one head to the next is almost 2^30 bytes (heads two at a time), and that long (one at a time)."""
+    H, D, T = 2, 128, 300
+    small = filled((1, 1, H, D), 304, [T], False, 30)
+    q = torch.randn((1, 1, 3 * H, 1, D), device=DEV).to(torch.bfloat16)
+    row = torch.randn((1, 1, 1, H, D), device=DEV).to(torch.bfloat16)
+    p = params((1, 1, H, D), 304, group=3)
+    outs = []
+    for rows in (304, (1 << 24) - 16, 1 << 24):
+        t = {}
+        for name in ("k", "v"):
+            t[name] = torch.empty((1, 1, H, rows, D // 2), dtype=torch.uint8, device=DEV)
+            t[name][:, :, :, :304] = small.t[name].to(DEV)
+            t[name + "_scale"] = torch.empty((1, 1, H, rows // BLOCK, D // GROUP, BLOCK), dtype=torch.uint8, device=DEV)
+            t[name + "_scale"][:, :, :, :19] = small.t[name + "_scale"].to(DEV)
+        view = B.cache_view(t["k"], t["v"], t["k_scale"], t["v_scale"])
+        B.ams_append(p, None, row, row, None, None, 0.0, None, None, lens_dev([T]), None, view)
+        out, w = torch.zeros_like(q), torch.zeros((H, 304), device=DEV)
+        B.ams_attend(p, view, lens_dev([T + 1]), q, out, torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV), None, None, w)
+        outs.append((out.float(), w))
+        del t, view
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    # the other kernel sums in another order: two roundings to bf16 of the same value may differ by one step, weights by the bound of a probability
+    assert (outs[0][0] - outs[2][0]).abs().max() <= 2.0 ** -7 * outs[0][0].abs().max()
+    assert ((outs[0][1] - outs[2][1]).abs() <= 2.0 ** -14 * outs[0][1] + 1e-30).all()
 
 
 # ---- together ---------------------------------------------------------------------------------------------------------
