@@ -1,15 +1,19 @@
 // Attention over a cache of 4 bits (ams_attend): the kernels of attend_kernel.h for its codes, and one that takes two heads at a time.
 //
 // A row of one head is 64 bytes (128 channels), half of a line: read head by head, a pool whose rows hold the heads side by side comes in
-// requests of half a line (256 ragged pairs of heads, 4096 to 16384 positions: 11.1 million requests of 64 bytes and 217 us, against
-// 5.6 million of 128 and 165 for slabs).  So, for up to 8 queries a head, a wave takes heads 2 i and 2 i + 1 together, and each of
+// requests of half a line (64 sequences of 4096 to 16384 positions and 8 heads: 11.1 million requests of 64 bytes and a pass of 266 us,
+// against 5.6 million of 128 and 209 for slabs).  So, for up to 8 queries a head, a wave takes heads 2 i and 2 i + 1 together, and each of
 // its loads both halves of a line:
 //   K of 16 positions as two tiles, (positions 0..7 of head 0, the same of head 1) and (positions 8..15 of head 1, the same of head 0); the
 //   columns are 8 queries of head 0 and 8 of head 1.  Half of either product is of one head's keys and the other's queries and is left out;
 //   the other halves lie in different lanes, so that one select per logit makes them 4 logits a lane, of its query and head.
 //   V as words P of positions 0..7 and Q of 8..15, lane groups 0, 1 of P and 2, 3 of Q holding head 0, the others head 1.  Each goes in as it
 //   is, with the probabilities of the other head's lanes set to 0: both heads' outputs in the same accumulators.
-// As many products as head by head, half of the work on logits.
+// As many products as head by head, half of the work on logits.  That pass takes 207 us (206 for slabs), of which 172 are this kernel: 819 MB at
+// 4.8 TB/s with the logits it writes.  What bounds it then is memory and how little of a stretch of 512 positions a workgroup spends at
+// that rate (the vector ALU is active for 45 %): with 1024 positions a workgroup 204 us and 150 instead of 164 without weights, but 66 instead of
+// 63 for 64 sequences of up to 4096, and 62 instead of 59 for 16 of up to 16384.  (512 workgroups that each take an even share of all
+// positions: 218; three waves on a SIMD: 218.)  64 channels: half lines also two heads at a time, 157 us against 134 for slabs.
 #include "attend_kernel.h"
 
 namespace ams {

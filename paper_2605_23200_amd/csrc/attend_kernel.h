@@ -1,4 +1,4 @@
-// Attention over a cache of 8 bits (ams_attend).
+// Attention over a cache of 8 or 4 bits (ams_attend): the kernels of one head.  (Joins and layouts: attend.hip; two heads a wave: attend_e2m1.hip.)
 //
 // One wave takes 32 positions at a time: K as 16x16x32 tiles with the positions as rows and the queries as columns,
 // S^T = K Q^T, so that a lane ends with 2 x 4 logits of ONE query (column lane % 16) at positions 4 (lane / 16) + 0..3 of both
@@ -20,8 +20,17 @@
 // vector ALU is active for 51 % and the matrix cores for 21 %.  (Sharing the conversions of four waves through
 // LDS: 52; the masks as a variant of the step: 44, but 128 against 120 for 64 units and 32 queries.)
 //
+// Codes of 4 bits: a quarter of a row of K is of one scale and in one lane, a conversion of two codes multiplies by the scale as well, and the
+// values are bf16 numbers, so that logits and probabilities need no factors; the rest is the same.  64 ragged sequences of up to 16384
+// positions and 14 queries a head in pages: 371 us, 314 in slabs (half lines, see attend_e2m1.hip); 8 units of 32768 and 128 queries: 39 us (345 vector
+// instructions for 32 positions and 32 queries, vector ALU 57 %, matrix cores 28 %; with 64 queries a wave 54; with three waves on a SIMD,
+// which spill 30 registers, a pass of 61 takes 67).  Not with the matrix cores' own scaled products of 4-bit by 8-bit floats, which take K's codes as they are: inside 32
+// channels their sums lose what lies about 2^14 below the largest product (5e-4 of it for codes of any size, measured), and queries would have
+// to go in as several terms of 4 bits.
+//
 // Weights: with up to 16 queries the logits go to scratch (4 N bytes a position, written and read once, against 2 D of K and V)
-// and the join turns them into probabilities; beyond that K is read a second time (attend_weights_kernel).
+// and the join turns them into probabilities; beyond that K is read a second time (attend_weights_kernel).  In 4 bits the same: with K again
+// for 9 to 16 queries 64 sequences of up to 16384 positions and 14 queries take 431 us against 365.
 #ifndef AMS_ATTEND_KERNEL_H
 #define AMS_ATTEND_KERNEL_H
 

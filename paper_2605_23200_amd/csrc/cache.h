@@ -1,4 +1,4 @@
-// Caches of 8 bits on the device: blocks, scales and codes (ams_cache in include/ams.h).
+// Caches of 8 and 4 bits on the device: blocks, scales and codes (ams_cache in include/ams.h).
 #ifndef AMS_CACHE_H
 #define AMS_CACHE_H
 
@@ -8,7 +8,7 @@
 
 namespace ams {
 
-constexpr int kBlockRows = 16;  // positions that share a scale; a page of the paged layout
+constexpr int kBlockRows = 16;  // positions that share a scale (in 4 bits: whose scales lie together); a page of the paged layout
 
 // Element types as the kernels are instantiated for them.
 enum { EL_F32 = AMS_F32, EL_BF16 = AMS_BF16, EL_INT8 = AMS_INT8, EL_E4M3 = AMS_E4M3, EL_E2M1 = AMS_E2M1 };

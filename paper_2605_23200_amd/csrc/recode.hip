@@ -1,4 +1,4 @@
-// Gather of cache rows between element types (ams_recode, ams_evict): rows of kv_dtype to 8 bits, 8 bits to rows, 8 bits to 8 bits, and
+// Gather of cache rows between element types (ams_recode, ams_evict): rows of kv_dtype to 8 or 4 bits, these to rows and among themselves, and
 // (ams_evict) rows of kv_dtype as they are.
 // value = code * scale of its block of 16 positions; a destination block takes the scale of the largest magnitude of ITS 16
 // rows, so a block is the unit of work: one wave holds all of it in registers (eight elements per lane and row: 16 lanes a
@@ -8,6 +8,11 @@
 // 2176 rows, 8 bits to 8 bits: 94 us with a wave for K and one for V that loaded row by row, 52 so (5.2 TB/s); 2048 of 32768 bf16 rows
 // to 8 bits: 96 and 83 (4.9 TB/s); 96 paged units, rows of 128 bytes scattered over a pool: 52 (3.9 TB/s).  Rows of kv_dtype as they
 // are: an eviction of 256 units to 2048 of 32768 takes 162 us, with a copy that went row by row 164.
+// 4 bits: a scale for every 32 channels of a row, which are four lanes; no two rows have anything in common.  2048 of 32768 bf16 rows, 256
+// units: 95 us, and 60 back to rows, 680 MB in all at 4.4 TB/s (92 with a conversion that does nothing, 47 without its stores: while it
+// reads, the memory-side cache writes back what the kernel before it wrote).  Four or five waves on a SIMD instead of eight win 3 % of that and
+// lose 2 % with whole slabs.  4 bits to 4 bits, 2048 of up to 16384 rows of 64 bytes scattered over a pool: 62 us with the write-back of 268 MB
+// (one, two and four rows a lane in flight: 151, 153 and 157 us for the eviction and its reading back).
 #include "cache.h"
 
 namespace ams {
