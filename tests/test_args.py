@@ -67,3 +67,33 @@ def test_one_stride_from_token_to_token():
             continue
         with pytest.raises(ValueError, match="one stride"):
             B._token_rows(v, shape, torch.float32, CPU, "k")
+
+
+def _nested(shape):
+    import warnings
+    with warnings.catch_warnings():
+        warnings.simplefilter("ignore")
+        return torch.nested.nested_tensor([torch.zeros(shape), torch.zeros((1,) + shape[1:])])
+
+
+def test_tensors_without_memory_of_their_own_are_refused():
+    """Asked for their sizes or their memory, these throw, or answer with none: an error here, not the end of the process."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    shape = (2, 2, 2, 1, 64)
+    with FakeTensorMode():
+        fake = torch.zeros(shape)
+    refused = []
+
+    def both(t):
+        for call in (lambda: B._arg(t, torch.float32, 4, CPU, "t"), lambda: B._token_rows(t, shape, torch.float32, CPU, "t")):
+            with pytest.raises(ValueError, match="expected"):
+                call()
+            refused.append(1)
+        return t
+
+    both(fake)
+    both(torch.zeros(shape, device="meta"))
+    both(_nested(shape[1:]))
+    torch.vmap(both)(torch.zeros((3,) + shape))
+    assert len(refused) == 8
+    assert B._arg(torch.zeros(0), torch.float32, 0, CPU, "t") == 0
