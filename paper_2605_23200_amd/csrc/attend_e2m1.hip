@@ -19,8 +19,8 @@
 namespace ams {
 namespace {
 
-// Not 0: a byte is 255.
-__device__ __forceinline__ uint32_t no_numbers(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & w & 0x80808080u; }
+// Not 0: a byte is 253 or more, a scale under which not every code is a finite bf16 number.
+__device__ __forceinline__ uint32_t beyond(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x03030303u) & w & 0x80808080u; }
 
 template <bool BF16, int HD>
 __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) {
@@ -178,8 +178,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
           vs[t][j] &= there == 4 ? 0xFFFFFFFFu : (1u << 8 * there) - 1;
         }
     }
-    if (__any((no_numbers(vs[0][0]) | no_numbers(vs[0][1]) | no_numbers(vs[1][0]) | no_numbers(vs[1][1])) != 0)) {
-      // channels of V that are no number: those of the queries that see the position, no others
+    if (__any((beyond(vs[0][0]) | beyond(vs[0][1]) | beyond(vs[1][0]) | beyond(vs[1][1])) != 0)) {
+      // Channels of V that are no number: those of the queries that see the position, no others.  Scales under which codes may be infinite: a
+      // quarter of them for the position's row, four times the probability, so that 0 times it stays 0.
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -188,6 +189,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
           const bool mine = (vs[t][j >> 2] >> shift & 255) == 255;
           const uint64_t bad = __ballot(mine);
           if (mine) vs[t][j >> 2] &= ~(255u << shift);
+          const uint32_t byte = vs[t][j >> 2] >> shift & 255;
+          if (__ballot(byte >= 253) >> 16 * g & 0xFFFF) {
+            vs[t][j >> 2] -= min(byte, 2u) << shift;
+            if (first_tile == (t == 0)) {
+              x[j] += 2.f;
+              sum -= 0.75f * power_of_two(x[j] - m);
+            }
+          }
           if (!bad) continue;
           bool hit = false;
 #pragma unroll

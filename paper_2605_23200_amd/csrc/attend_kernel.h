@@ -492,11 +492,21 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
       uint32_t most = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(vpower[j]));
-      if (__any(most == 0x7F800000u)) {  // channels of V that are no number: those of the queries that see the position, no others
+      // Channels of V that are no number: those of the queries that see the position, no others.  Scales from 2^126 on, under which codes may be
+      // infinite: a quarter of them for the position's row, four times the probability, so that 0 times it stays 0.
+      if (__any(most >= 0x7E800000u)) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const uint64_t bad = __ballot(__float_as_uint(vpower[j]) == 0x7F800000u);
           if (__float_as_uint(vpower[j]) == 0x7F800000u) vpower[j] = 0.f;
+          if (__ballot(__float_as_uint(vpower[j]) >= 0x7E800000u) >> 16 * g & 0xFFFF) {
+            vpower[j] = __uint_as_float(max(__float_as_uint(vpower[j]), 2u << 23) - (2u << 23));
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              x[r][j] += RAW ? 2.f / to_log2 : 2.f;
+              sum[r] -= 0.75f * power_of_two((RAW ? x[r][j] * to_log2 : x[r][j]) - m[r]);
+            }
+          }
           if (!bad) continue;
 #pragma unroll
           for (int r = 0; r < R; ++r) {

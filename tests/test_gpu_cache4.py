@@ -472,6 +472,61 @@ def test_attend_nan_scales(heads, D, group, W, dtype):
             assert not torch.isnan(w[b * heads + h]).any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads", [1, 2])
+@pytest.mark.parametrize("group,W", [(2, 4), (1, 16), (2, 24)])
+def test_attend_values_at_the_end_of_the_range(heads, D, group, W, dtype):
+    """Scales of 2^126 and 2^127 of V.  Codes under them that are finite count as they are (one step of positions: no probability above 1, no sum
+    above the largest value); codes that are not are the business of the queries that see them, not of other queries, channels or heads."""
+    lens = [30, 17]
+    cache = filled((1, 2, heads, D), 40, lens, heads == 2, 14)
+    rng = np.random.default_rng(15)
+    for b, t, part, byte in ((0, 28, 0, 254), (0, 27, D // GROUP - 1, 253), (1, 3, 0, 253)):
+        codes, scales = cache.get("v", 0, b, heads - 1, t)
+        codes[part * GROUP:(part + 1) * GROUP], scales[part] = rng.integers(0, 4, GROUP), byte
+        cache.put("v", 0, b, heads - 1, t, codes, scales)
+    _attend_case(cache, lens, group, W, dtype, causal=True)
+
+    lens = [160, 147]
+    cache = filled((1, 2, heads, D), 200, lens, heads == 2, 16)
+    plain, sees = cache.copy(), np.zeros((2, heads, W, D), dtype=bool)
+    for b, T in enumerate(lens):
+        for h, (back, part, byte) in enumerate(((2, 0, 253), (1, D // GROUP - 1, 254))[:heads]):
+            codes, scales = cache.get("v", 0, b, h, T - back)
+            codes[part * GROUP:(part + 1) * GROUP], scales[part] = 7, byte
+            cache.put("v", 0, b, h, T - back, codes, scales)
+            sees[b, h] = (np.arange(W) >= W - back)[:, None]
+    p = params((1, 2, heads, D), 200, group=group, window=W, causal=True, dtype=dtype)
+    q = torch.randn((1, 2, heads * group, W, D), generator=torch.Generator().manual_seed(3)).to(ROWS[dtype]).to(DEV)
+    got = []
+    for c in (cache, plain):
+        out, w = torch.zeros_like(q), torch.zeros((2 * heads, 200), device=DEV)
+        B.ams_attend(p, c.upload(), lens_dev(lens), q, out, torch.zeros(B.ams_attend_workspace_bytes(p), dtype=torch.uint8, device=DEV), None, None, w)
+        got.append((out.cpu().view(2, heads, group, W, D), w))
+    # The weights do not know V, but that the sum of a query that sees such a row is (sum - 3/4 y) + y, y = 2^(x + 2), for sum + 2^x: 2^-24 |x + 2|
+    # of y from the rounding of x + 2, 2^-22 each of at most 4 sums from the two roundings, where the sum stays.
+    logits = max(float(np.abs(q[0, b, h * group:(h + 1) * group].reshape(-1, D).double().cpu().numpy() @ cache.rows("k", 0, b, h, lens[b]).T).max())
+                 for b in range(2) for h in range(heads)) / D ** 0.5 * 1.4427
+    assert ((got[0][1] - got[1][1]).abs() <= (2.0 ** -24 * (logits + 2) + 2.0 ** -20) * got[1][1]).all()
+    for b in range(2):
+        for h in range(heads):
+            for g in range(group):
+                other = torch.from_numpy(~sees[b, h])
+                same_bits(got[0][0][b, h, g][other], got[1][0][b, h, g][other])
+            # Who sees it: what lies in the other channels is what it was, but for the position's probability (the bits of x + 2, a quarter of the
+            # scale: 2^-17 of it in either as two bf16 terms, and less from the exponential) and the rounding of both outputs.
+            for g in range(group):
+                x, y = got[0][0][b, h, g].double(), got[1][0][b, h, g].double()
+                part = slice(GROUP, None) if h == 0 else slice(0, D - GROUP)
+                step = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -17
+                assert ((x - y).abs()[:, part] <= step * y.abs()[:, part] + 2.0 ** -15 * cache_top(plain, b, h, lens[b])).all(), (b, h, g)
+
+
+def cache_top(cache, b, h, T):
+    return float(np.abs(cache.rows("v", 0, b, h, T)).max())
+
+
 @pytest.mark.parametrize("heads", [1, 2])
 @pytest.mark.parametrize("W", [3, 4, 24])
 def test_attend_a_query_that_is_no_number(heads, W):
