@@ -346,7 +346,7 @@ int ams_compress_step(const ams_params* p, const ams_kv_view* src, const int32_t
  * largest magnitude of the 32 to 7 or less (0 for zeros, 255 for a value that is infinite or no number, both with codes of 0), the code the
  * nearest to value / scale, of two equally near ones the even one: no code is off by more than half of the steps between 4 and 6.  A row's
  * codes depend on that row alone: what is in the cache is never rounded again.  The readers take any byte (0 is 2^-127); a code that stands for
- * 2^128 or more (bytes 253 and 254; a finite row gives one from 1.75 * 2^127 on) is read as infinite, or makes what sees it infinite or no number.
+ * 2^128 or more (bytes 253 and 254; a finite row gives one from 1.75 * 2^127 on) is read as infinite, but as itself in sums over V.
  * A block table entry outside the pool is read as the nearest page and never written through.  Blocks
  * that a call writes belong to one (sequence, place in the table) alone.
  * Outputs of the calls below overlap neither inputs nor one another unless it says so; calls that overlap in

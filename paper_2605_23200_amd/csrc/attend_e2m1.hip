@@ -14,6 +14,8 @@
 // that rate (the vector ALU is active for 45 %): with 1024 positions a workgroup 204 us and 150 instead of 164 without weights, but 66 instead of
 // 63 for 64 sequences of up to 4096, and 62 instead of 59 for 16 of up to 16384.  (512 workgroups that each take an even share of all
 // positions: 218; three waves on a SIMD: 218.)  64 channels: half lines also two heads at a time, 157 us against 134 for slabs.
+// 9 to 16 queries a head: the same tiles of K with the 16 columns of either head in turn, P and Q likewise: twice the products, none of the
+// logits wasted.  64 ragged sequences of up to 16384 positions and 14 queries: a pass of 321 us, 362 head by head (306 in slabs).
 #include "attend_kernel.h"
 
 namespace ams {
@@ -22,7 +24,8 @@ namespace {
 // Not 0: a byte is 253 or more, a scale under which not every code is a finite bf16 number.
 __device__ __forceinline__ uint32_t beyond(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x03030303u) & w & 0x80808080u; }
 
-template <bool BF16, int HD>
+// SETS of columns: 1, 8 queries of either head; 2, 16 of each.
+template <bool BF16, int HD, int SETS>
 __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) {
   constexpr int STEPS = HD / 32, TILES = HD / 16, TERMS = BF16 ? 1 : 3, PTERMS = BF16 ? 2 : 3;
   constexpr int LD = HD + 4;
@@ -30,25 +33,34 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
   __shared__ float2 stat[kWaves][16];
   const int unit0 = 2 * blockIdx.y, split = turned_x();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int g = lane >> 4, c = lane & 15, head = c >> 3, n = c & 7, gg = g ^ (2 * head);  // the lane's query, and where its positions lie
-  const bool first_tile = (g < 2) == (head == 0);
+  const int g = lane >> 4, c = lane & 15, n = SETS == 1 ? c & 7 : c;  // the lane's query
+  auto head_of = [&](int set) __attribute__((always_inline)) { return SETS == 1 ? c >> 3 : set; };
+  auto first_tile = [&](int set) __attribute__((always_inline)) { return (g < 2) == (head_of(set) == 0); };
+  auto group = [&](int set) __attribute__((always_inline)) { return g ^ (2 * head_of(set)); };  // its four positions of a block
   int l, b, h;
   unit_coords(a.d, unit0, l, b, h);
   const int T = seq_len(a.d, a.seq_lens, b), N = a.d.N;
   const int begin = split * a.chunk, end = min(T, begin + a.chunk);
   if (begin >= T && split > 0) return;  // the join knows; split 0 of an empty sequence writes the zeros
-  bf16x8 q[STEPS][TERMS];
+  bf16x8 q[SETS][STEPS][TERMS];
   {
     // (rows of the pair's second head follow the first's)
     const char* of_pair = a.q + (int64_t)unit0 * N * HD * (BF16 ? 2 : 4);
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) Queries<EL_E2M1, BF16, HD, 1>::load_one(of_pair, n < N ? head * N + n : 2 * N, 2 * N, i, lane, q[i]);
+    for (int set = 0; set < SETS; ++set)
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i)
+        Queries<EL_E2M1, BF16, HD, 1>::load_one(of_pair, n < N ? head_of(set) * N + n : 2 * N, 2 * N, i, lane, q[set][i]);
   }
   const int limit = a.causal ? T - a.d.W + 1 + n % a.d.W : T, fewest = a.causal ? T - a.d.W + 1 : T;
-  floatx4 o[TILES];
-  float m = kLowest, sum = 0.f;
+  floatx4 o[SETS][TILES];
+  float m[SETS], sum[SETS];
 #pragma unroll
-  for (int e = 0; e < TILES; ++e) o[e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int set = 0; set < SETS; ++set) {
+    m[set] = kLowest, sum[set] = 0.f;
+#pragma unroll
+    for (int e = 0; e < TILES; ++e) o[set][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
   const float to_log2 = kLog2E / sqrtf((float)HD);
   const UnitBlocks<EL_E2M1, HD> u(a.k, a.v, l, b, h);
   const uint32_t head_stride = a.k.paged ? HD / 2 : (uint32_t)(a.k.t_capacity * (HD / 2));
@@ -59,7 +71,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
   uint32_t k_at[2], ks_at[2], v_at[2], vs_at[2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int k_head = head ^ t, v_head = (g >> 1) ^ t, k_row = 8 * t + n, v_row = 8 * t + 4 * (g & 1);
+    const int k_head = (c >> 3) ^ t, v_head = (g >> 1) ^ t, k_row = 8 * t + (c & 7), v_row = 8 * t + 4 * (g & 1);
     k_at[t] = k_row * row_stride + k_head * head_stride + g * (HD / 8);
     ks_at[t] = k_head * head_scales + micro_at<HD>(g * (HD / 4), k_row);
     v_at[t] = v_row * row_stride + v_head * head_stride + c * (HD / 32);
@@ -84,7 +96,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
       const int most = T - 1 - min(at / kBlockRows + j, last_blk) * kBlockRows;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint32_t past = CLAMP ? max(8 * t + n - most, 0) : 0;
+        const uint32_t past = CLAMP ? max(8 * t + (c & 7) - most, 0) : 0;
         const char* from = block + (k_at[t] - past * row_stride);
         if constexpr (HD == 128) {
           const uint4 x = *(const uint4*)from;
@@ -126,22 +138,27 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
   // One step.  MORE: there is another, whose K is loaded when this one's has been used, V likewise; CLAMP: it is the wave's last.
   auto step = [&](auto more, auto clamp) __attribute__((always_inline)) {
     constexpr bool MORE = decltype(more)::value;
-    float x[8];
+    float x[SETS][8];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      floatx4 s[2];
+      floatx4 s[SETS][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int set = 0; set < SETS; ++set) s[set][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
           const bf16x8 k = eight_of_four_bits(kw[j][t][i], ks[j][t]);
 #pragma unroll
-          for (int r = TERMS - 1; r >= 0; --r) s[t] = mma(k, q[i][r], s[t]);
+          for (int set = 0; set < SETS; ++set)
+#pragma unroll
+            for (int r = TERMS - 1; r >= 0; --r) s[set][t] = mma(k, q[set][i][r], s[set][t]);
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * j + i] = (first_tile ? s[0][i] : s[1][i]) * to_log2;
+      for (int set = 0; set < SETS; ++set)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[set][4 * j + i] = (first_tile(set) ? s[set][0][i] : s[set][1][i]) * to_log2;
     }
     const int next = at + stride;
     if constexpr (MORE) {
@@ -151,23 +168,37 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
     }
     if (at + kStep > fewest) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (at + (j >> 2) * 16 + 4 * gg + (j & 3) >= limit) x[j] = -INFINITY;
+      for (int set = 0; set < SETS; ++set)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (at + (j >> 2) * 16 + 4 * group(set) + (j & 3) >= limit) x[set][j] = -INFINITY;
     }
-    float top = -INFINITY;
+    float top[SETS];
+    bool higher = false;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
-    if (__any(top > m + kSlack)) {
-      const float now = fmaxf(m, query_max(top)), shrink = power_of_two(m - now);
-      m = now;
-      sum *= shrink;
+    for (int set = 0; set < SETS; ++set) {
+      top[set] = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < TILES; ++e) o[e] *= shrink;
+      for (int j = 0; j < 8; ++j) top[set] = fmaxf(top[set], x[set][j]);
+      higher = higher || top[set] > m[set] + kSlack;
+    }
+    if (__any(higher)) {
+#pragma unroll
+      for (int set = 0; set < SETS; ++set) {
+        const float now = fmaxf(m[set], query_max(top[set])), shrink = power_of_two(m[set] - now);
+        m[set] = now;
+        sum[set] *= shrink;
+#pragma unroll
+        for (int e = 0; e < TILES; ++e) o[set][e] *= shrink;
+      }
     }
     if (a.stash && n < N) {
-      float* to = a.stash + (((int64_t)(unit0 + head) * ((a.d.t_max + 15) / 16) + at / 16) * N + n) * 16 + 4 * gg;
-      *(float4*)to = make_float4(x[0], x[1], x[2], x[3]);
-      if (at + 16 < T) *(float4*)(to + N * 16) = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+      for (int set = 0; set < SETS; ++set) {
+        float* to = a.stash + (((int64_t)(unit0 + head_of(set)) * ((a.d.t_max + 15) / 16) + at / 16) * N + n) * 16 + 4 * group(set);
+        *(float4*)to = make_float4(x[set][0], x[set][1], x[set][2], x[set][3]);
+        if (at + 16 < T) *(float4*)(to + N * 16) = make_float4(x[set][4], x[set][5], x[set][6], x[set][7]);
+      }
     }
     if constexpr (!MORE) {  // (the sequence's end lies in a last step)
 #pragma unroll
@@ -192,41 +223,47 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
           const uint32_t byte = vs[t][j >> 2] >> shift & 255;
           if (__ballot(byte >= 253) >> 16 * g & 0xFFFF) {
             vs[t][j >> 2] -= min(byte, 2u) << shift;
-            if (first_tile == (t == 0)) {
-              x[j] += 2.f;
-              sum -= 0.75f * power_of_two(x[j] - m);
-            }
+#pragma unroll
+            for (int set = 0; set < SETS; ++set)
+              if (first_tile(set) == (t == 0)) {
+                x[set][j] += 2.f;
+                sum[set] -= 0.75f * power_of_two(x[set][j] - m[set]);
+              }
           }
           if (!bad) continue;
-          bool hit = false;
 #pragma unroll
-          for (int i = 0; i < 2; ++i)  // lane groups that hold the lane's head, channels of the scale that its outputs have
-            hit = hit || ((bad >> (16 * (2 * (head ^ t) + i) + 4 * g * TILES / 32 * (32 / TILES)) & 1) &&
-                          at + 16 * (j >> 2) + 8 * t + 4 * i + (j & 3) < limit);
-          const float no_number = hit ? __uint_as_float(0x7FC00000u) : 0.f;
+          for (int set = 0; set < SETS; ++set) {
+            bool hit = false;
 #pragma unroll
-          for (int e = 0; e < TILES; ++e) o[e] += no_number;
+            for (int i = 0; i < 2; ++i)  // lane groups that hold the column's head, channels of the scale that its outputs have
+              hit = hit || ((bad >> (16 * (2 * (head_of(set) ^ t) + i) + 4 * g * TILES / 32 * (32 / TILES)) & 1) &&
+                            at + 16 * (j >> 2) + 8 * t + 4 * i + (j & 3) < limit);
+            const float no_number = hit ? __uint_as_float(0x7FC00000u) : 0.f;
+#pragma unroll
+            for (int e = 0; e < TILES; ++e) o[set][e] += no_number;
+          }
         }
     }
     // From here on nothing branches: exponentials, conversions and products can be mixed.
-    bf16x8 p[2][PTERMS];
-    {
+    bf16x8 p[SETS][2][PTERMS];
+#pragma unroll
+    for (int set = 0; set < SETS; ++set) {
       uint32_t t[3][4];
 #pragma unroll
       for (int j = 0; j < 8; j += 2) {
-        float p0 = power_of_two(x[j] - m), p1 = power_of_two(x[j + 1] - m);
-        sum += p0 + p1;
+        float p0 = power_of_two(x[set][j] - m[set]), p1 = power_of_two(x[set][j + 1] - m[set]);
+        sum[set] += p0 + p1;
 #pragma unroll
         for (int k = 0; k < PTERMS; ++k) {
           t[k][j >> 1] = bf16_pair(p0, p1);
           if (k + 1 < PTERMS) p0 -= __uint_as_float(t[k][j >> 1] << 16), p1 -= __uint_as_float(t[k][j >> 1] & 0xFFFF0000u);
         }
       }
-      const uint32_t in_p = first_tile ? 0xFFFFFFFFu : 0u, in_q = ~in_p;
+      const uint32_t in_p = first_tile(set) ? 0xFFFFFFFFu : 0u, in_q = ~in_p;
 #pragma unroll
       for (int k = 0; k < PTERMS; ++k) {
-        p[0][k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0] & in_p, t[k][1] & in_p, t[k][2] & in_p, t[k][3] & in_p));
-        p[1][k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0] & in_q, t[k][1] & in_q, t[k][2] & in_q, t[k][3] & in_q));
+        p[set][0][k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0] & in_p, t[k][1] & in_p, t[k][2] & in_p, t[k][3] & in_p));
+        p[set][1][k] = __builtin_bit_cast(bf16x8, make_uint4(t[k][0] & in_q, t[k][1] & in_q, t[k][2] & in_q, t[k][3] & in_q));
       }
     }
 #pragma unroll
@@ -238,9 +275,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
         bf16x8 e[2];
         turn_pair(vw[t], power, w, e[0], e[1]);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int set = 0; set < SETS; ++set)
 #pragma unroll
-          for (int r = PTERMS - 1; r >= 0; --r) o[2 * w + k] = mma(e[k], p[t][r], o[2 * w + k]);
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = PTERMS - 1; r >= 0; --r) o[set][2 * w + k] = mma(e[k], p[set][t][r], o[set][2 * w + k]);
       }
     }
     if constexpr (MORE) load_v(clamp, next);
@@ -256,36 +295,46 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
     step(std::false_type{}, std::true_type{});
   }
   // the waves together: thread (column, stretch of HD / 16 channels)
-  const float total = query_sum(sum);
-  if (g == 0) stat[wave][c] = make_float2(m, total);
 #pragma unroll
-  for (int q4 = 0; q4 < 4; ++q4)
+  for (int set = 0; set < SETS; ++set) {
+    if (set > 0) __syncthreads();
+    const float total = query_sum(sum[set]);
+    if (g == 0) stat[wave][c] = make_float2(m[set], total);
 #pragma unroll
-    for (int e = 0; e < TILES; e += 4)
-      *(float4*)&joint[wave][c][TILES * (4 * g + q4) + e] = make_float4(o[e][q4], o[e + 1][q4], o[e + 2][q4], o[e + 3][q4]);
-  __syncthreads();
-  const int column = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * TILES;
-  if ((column & 7) >= N) return;
-  float highest = stat[0][column].x;
+    for (int q4 = 0; q4 < 4; ++q4)
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) highest = fmaxf(highest, stat[w][column].x);
-  float y[TILES], all = 0.f;
+      for (int e = 0; e < TILES; e += 4)
+        *(float4*)&joint[wave][c][TILES * (4 * g + q4) + e] = make_float4(o[set][e][q4], o[set][e + 1][q4], o[set][e + 2][q4], o[set][e + 3][q4]);
+    __syncthreads();
+    const int column = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * TILES, of = SETS == 1 ? column & 7 : column;
+    if (of >= N) continue;
+    float highest = stat[0][column].x;
 #pragma unroll
-  for (int e = 0; e < TILES; ++e) y[e] = 0.f;
+    for (int w = 1; w < kWaves; ++w) highest = fmaxf(highest, stat[w][column].x);
+    float y[TILES], all = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float f = power_of_two(stat[w][column].x - highest);
-    all = fmaf(f, stat[w][column].y, all);
+    for (int e = 0; e < TILES; ++e) y[e] = 0.f;
 #pragma unroll
-    for (int e = 0; e < TILES; ++e) y[e] = fmaf(f, joint[w][column][d0 + e], y[e]);
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = power_of_two(stat[w][column].x - highest);
+      all = fmaf(f, stat[w][column].y, all);
+#pragma unroll
+      for (int e = 0; e < TILES; ++e) y[e] = fmaf(f, joint[w][column][d0 + e], y[e]);
+    }
+    finish_query<BF16, HD>(a, unit0 + (SETS == 1 ? column >> 3 : set), of, split, highest, all, y, d0);
   }
-  finish_query<BF16, HD>(a, unit0 + (column >> 3), column & 7, split, highest, all, y, d0);
 }
 
 template <bool BF16, int HD>
 hipError_t launch_pairs(const AttendArgs& a, const AttendLayout& lay, hipStream_t s) {
+  const dim3 grid(lay.n_splits, a.d.units / 2);
   prof_mark("attend", s);
-  hipLaunchKernelGGL((attend_pair_kernel<BF16, HD>), dim3(lay.n_splits, a.d.units / 2), dim3(kThreads), 0, s, a);
+  if (a.d.N <= 8)
+    hipLaunchKernelGGL((attend_pair_kernel<BF16, HD, 1>), grid, dim3(kThreads), 0, s, a);
+  else if constexpr (BF16 && HD == 128)
+    hipLaunchKernelGGL((attend_pair_kernel<BF16, HD, 2>), grid, dim3(kThreads), 0, s, a);
+  else
+    return hipErrorNotSupported;
   if (lay.n_splits > 1 || a.stash) launch_attend_join(a, lay, BF16, s);
   return hipGetLastError();
 }

@@ -21,8 +21,8 @@
 // LDS: 52; the masks as a variant of the step: 44, but 128 against 120 for 64 units and 32 queries.)
 //
 // Codes of 4 bits: a quarter of a row of K is of one scale and in one lane, a conversion of two codes multiplies by the scale as well, and the
-// values are bf16 numbers, so that logits and probabilities need no factors; the rest is the same.  64 ragged sequences of up to 16384
-// positions and 14 queries a head in pages: 371 us, 314 in slabs (half lines, see attend_e2m1.hip); 8 units of 32768 and 128 queries: 39 us (345 vector
+// values are bf16 numbers, so that logits and probabilities need no factors; the rest is the same.  (Up to 16 queries: attend_e2m1.hip.)  64
+// ragged sequences of up to 16384 positions and 14 queries a head in slabs: 306 us; 8 units of 32768 and 128 queries: 39 us (345 vector
 // instructions for 32 positions and 32 queries, vector ALU 57 %, matrix cores 28 %; with 64 queries a wave 54; with three waves on a SIMD,
 // which spill 30 registers, a pass of 61 takes 67).  Not with the matrix cores' own scaled products of 4-bit by 8-bit floats, which take K's codes as they are: inside 32
 // channels their sums lose what lies about 2^14 below the largest product (5e-4 of it for codes of any size, measured), and queries would have

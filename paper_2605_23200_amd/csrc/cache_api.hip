@@ -58,8 +58,17 @@ bool same_slab(const ams_cache* a, const ams_cache* b) {  // paged views may sha
 
 // Heads two at a time: up to 8 queries a head, rows of 4 bits whose offsets from one head to the next are of 32 bits.  (Paged, 64 ragged
 // sequences of up to 16384 positions and 8 heads: a pass of 207 us, 266 head by head; 4 sequences of 16384: 24 and 34; slabs: 206 and 210.)
+// 9 to 16 bf16 queries over 128 channels: in pages, where there are positions enough.  (16 queries and 8 heads in pages, two heads and one: 64
+// ragged sequences of up to 16384 positions 321 and 362 us with 14 queries; 64 of 2177 69 and 93, of 1000 35 and 41, of 300 19.7 and 18.9;
+// 8 of 4096 23.9 and 26.3, of 2177 21.1 and 19.5; one of 32768 23.4 and 25.3, of 16384 18.0 and 17.9, of 4096 13.8 and 12.5; slabs: 317
+// and 306 for the first.)
 bool in_pairs(const ams_params* p, const ams_cache* c) {
-  if (!micro(c) || p->n_kv_heads % 2 || (int64_t)p->group * p->window > 8) return false;
+  if (!micro(c) || p->n_kv_heads % 2) return false;
+  const int64_t n = (int64_t)p->group * p->window;
+  if (n > 8) {
+    if (n > 16 || p->kv_dtype != AMS_BF16 || p->head_dim != 128 || c->kv.layout != AMS_LAYOUT_PAGED) return false;
+    return (int64_t)p->n_layers * p->batch * p->n_kv_heads * p->t_max >= 1 << 18;
+  }
   return c->kv.layout == AMS_LAYOUT_PAGED || c->kv.t_capacity < (1 << 24);
 }
 
