@@ -673,16 +673,18 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, 
   };
   int first = start + wave * BLOCKS * kBlockRows;
   fetch(first);
-  {  // joined, or of the only split; a query that is not there counts nothing
+  // Joined, or of the only split.  In the places of the last 32 that have no query stands the last one again, counted 0: its probabilities are
+  // numbers wherever its own are, also under keys that are infinite (zeros in its place would make the weights there NaN).
+  {
     const int n = row_begin + threadIdx.x;
-    const float2 st = n < row_end ? a.joined[(int64_t)unit * N + n] : make_float2(0.f, 0.f);
-    stat[threadIdx.x] = make_float2(st.x, st.y == 0.f ? 0.f : 1.f / st.y);
+    const float2 st = a.joined[(int64_t)unit * N + min(n, row_end - 1)];
+    stat[threadIdx.x] = make_float2(st.x, n >= row_end || st.y == 0.f ? 0.f : 1.f / st.y);
   }
   const char* unit_q = a.q + (int64_t)unit * N * HD * (BF16 ? 2 : 4);
   for (int f = wave; f < groups * R * STEPS; f += kWaves) {
     const int group = f / (R * STEPS), r = f / STEPS % R, i = f % STEPS;
     bf16x8 one[TERMS];
-    Queries<EL, BF16, HD, R>::load_one(unit_q, row_begin + group * kWeightRows + r * 16 + c, row_end, i, lane, one);
+    Queries<EL, BF16, HD, R>::load_one(unit_q, min(row_begin + group * kWeightRows + r * 16 + c, row_end - 1), row_end, i, lane, one);
 #pragma unroll
     for (int t = 0; t < TERMS; ++t) q[group][r][i][t][lane] = one[t];
   }
