@@ -427,7 +427,7 @@ size_t ams_evict_workspace_bytes(const ams_params* p);
  *   s[n][t] = q_n . k_t / sqrt(D), p = softmax over the positions that n sees, out_n = sum_t p[n][t] v_t,
  *   lse_n = ln sum_t exp(s[n][t]),  weights_out[t] = weights_in[t] + sum_n p[n][t]   (n: the unit's G * W queries)
  * p->causal == 0: every query sees 0 .. T-1; 1: query w sits at T-W+w and sees 0 .. T-W+w.  A query that sees nothing
- * (T = 0; before position 0) has out 0 and lse -inf and adds no weight.
+ * (T = 0; before position 0), or whose every logit is -inf, has out 0 and lse -inf and adds no weight.
  * Of p: the sizes, kv_dtype (of q and out), causal, t_max, t_stride; group * window <= 256 (AMS_ERR_UNSUPPORTED).
  *   src   AMS_INT8, AMS_E4M3 or AMS_E2M1 (AMS_ERR_UNSUPPORTED otherwise)
  *   q     [dev] [layers, batch, kv_heads * group, window, head_dim] kv_dtype; out likewise, written

@@ -142,19 +142,24 @@ __global__ __launch_bounds__(kThreads, 2) void attend_pair_kernel(AttendArgs a) 
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       floatx4 s[SETS][2];
+      auto products = [&](auto ends) __attribute__((always_inline)) {  // ends: of the range of K
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int set = 0; set < SETS; ++set) s[set][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+          for (int set = 0; set < SETS; ++set) s[set][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-          const bf16x8 k = eight_of_four_bits(kw[j][t][i], ks[j][t]);
+          for (int i = 0; i < STEPS; ++i) {
+            const bf16x8 k = eight_of_four_bits(kw[j][t][i], ks[j][t]), low = decltype(ends)::value ? without_infinite(k) : k;
 #pragma unroll
-          for (int set = 0; set < SETS; ++set)
+            for (int set = 0; set < SETS; ++set)
 #pragma unroll
-            for (int r = TERMS - 1; r >= 0; --r) s[set][t] = mma(k, q[set][i][r], s[set][t]);
+              for (int r = TERMS - 1; r >= 0; --r) s[set][t] = mma(r > 0 ? low : k, q[set][i][r], s[set][t]);
+          }
         }
-      }
+      };
+      products(std::false_type{});
+      if constexpr (TERMS > 1)
+        if (__any(max(__float_as_uint(ks[j][0]), __float_as_uint(ks[j][1])) >= kBeyond)) products(std::true_type{});
 #pragma unroll
       for (int set = 0; set < SETS; ++set)
 #pragma unroll

@@ -76,6 +76,20 @@ __device__ __forceinline__ uint32_t two_of_four_bits(uint32_t w, float scale, in
   }
   return __builtin_bit_cast(uint32_t, c);
 }
+// Scale bytes of 253 and 254: codes under them may be infinite as bf16.
+constexpr uint32_t kBeyond = 253u << 23;  // as the scale's bits
+// Those of an operand as 0.  Queries of fp32 go in as three terms, of which the lower ones may be 0 or have the other sign: times an infinite
+// key they would make a logit no number that the first term makes infinite.  (So products are formed in two ways, by whether a step holds such
+// a scale: 8 units of 16384 and 128 queries 65.5 -> 66.2 us, 16.4 us and less no difference.)
+__device__ __forceinline__ bf16x8 without_infinite(bf16x8 x) {
+  uint4 r = __builtin_bit_cast(uint4, x);
+  asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w));  // (formed where it is used: kept over a loop it would take 64 registers)
+  auto one = [](uint32_t w) __attribute__((always_inline)) {
+    return w & ((w & 0x7FFFu) == 0x7F80u ? 0xFFFF0000u : 0xFFFFFFFFu) & ((w & 0x7FFF0000u) == 0x7F800000u ? 0xFFFFu : 0xFFFFFFFFu);
+  };
+  r = make_uint4(one(r.x), one(r.y), one(r.z), one(r.w));
+  return __builtin_bit_cast(bf16x8, r);
+}
 // Eight codes -> the operand of one product.
 template <int EL>
 __device__ __forceinline__ bf16x8 eight_codes(uint32_t lo, uint32_t hi) {
@@ -426,20 +440,25 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
     const bool whole = at + kStep <= fewest;  // every query sees every position of the step
     floatx4 s[2][R];
     float kscale[2];
+    auto products = [&](auto ends) __attribute__((always_inline)) {  // ends: of the range of K
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      kscale[j] = kt[j].of_logits() * to_log2;
+      for (int j = 0; j < 2; ++j) {
+        kscale[j] = kt[j].of_logits() * to_log2;
 #pragma unroll
-      for (int r = 0; r < R; ++r) s[j][r] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < R; ++r) s[j][r] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const bf16x8 k = kt[j].operand(i);
+        for (int i = 0; i < STEPS; ++i) {
+          const bf16x8 k = kt[j].operand(i), low = decltype(ends)::value ? without_infinite(k) : k;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+          for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int t = TERMS - 1; t >= 0; --t) s[j][r] = mma(k, q.x[r][i][t], s[j][r]);
+            for (int t = TERMS - 1; t >= 0; --t) s[j][r] = mma(t > 0 ? low : k, q.x[r][i][t], s[j][r]);
+        }
       }
-    }
+    };
+    products(std::false_type{});
+    if constexpr (kMicro<EL> && TERMS > 1)
+      if (__any(max(__float_as_uint(kt[0].scale), __float_as_uint(kt[1].scale)) >= kBeyond)) products(std::true_type{});
     const int next = at + stride;
     if constexpr (MORE) {
       settle(next);
@@ -701,45 +720,58 @@ __global__ __launch_bounds__(kThreads) void attend_weights_kernel(AttendArgs a, 
       scale[j] = k[j].of_logits() * to_log2;
       w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0.f;
     }
+    bool ends = false;  // of the range of K
+    if constexpr (kMicro<EL> && TERMS > 1) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int j = 0; j < BLOCKS; ++j) most = max(most, __float_as_uint(k[j].scale));
+      ends = __any(most >= kBeyond);
+    }
     fetch(first + STEP);
     const bool whole = first + BLOCKS * kBlockRows <= fewest;
-    for (int group = 0; group < groups; ++group) {
-      floatx4 s[BLOCKS][R];
+    auto queries = [&](auto ends) __attribute__((always_inline)) {
+      for (int group = 0; group < groups; ++group) {
+        floatx4 s[BLOCKS][R];
 #pragma unroll
-      for (int j = 0; j < BLOCKS; ++j)
+        for (int j = 0; j < BLOCKS; ++j)
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[j][r] = floatx4{0.f, 0.f, 0.f, 0.f};
+          for (int r = 0; r < R; ++r) s[j][r] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i)
+        for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+          for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int t = TERMS - 1; t >= 0; --t) {
-            const bf16x8 y = q[group][r][i][t][lane];
+            for (int t = TERMS - 1; t >= 0; --t) {
+              const bf16x8 y = q[group][r][i][t][lane];
 #pragma unroll
-            for (int j = 0; j < BLOCKS; ++j) s[j][r] = mma(x[j][i], y, s[j][r]);
-          }
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int m = group * kWeightRows + r * 16 + c, n = row_begin + m;
-        const float2 st = stat[m];
-        if (whole) {
-#pragma unroll
-          for (int j = 0; j < BLOCKS; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[j][i] = fmaf(power_of_two(fmaf(s[j][r][i], scale[j], -st.x)), st.y, w[j][i]);
-        } else {
-          const int limit = n >= row_end ? 0 : a.causal ? T - a.d.W + 1 + n % a.d.W : T;
-#pragma unroll
-          for (int j = 0; j < BLOCKS; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float p = power_of_two(fmaf(s[j][r][i], scale[j], -st.x)) * st.y;
-              if (first + 16 * j + 4 * g + i < limit) w[j][i] += p;
+              for (int j = 0; j < BLOCKS; ++j) s[j][r] = mma(decltype(ends)::value && t > 0 ? without_infinite(x[j][i]) : x[j][i], y, s[j][r]);
             }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int m = group * kWeightRows + r * 16 + c, n = row_begin + m;
+          const float2 st = stat[m];
+          if (whole) {
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) w[j][i] = fmaf(power_of_two(fmaf(s[j][r][i], scale[j], -st.x)), st.y, w[j][i]);
+          } else {
+            const int limit = n >= row_end ? 0 : a.causal ? T - a.d.W + 1 + n % a.d.W : T;
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float p = power_of_two(fmaf(s[j][r][i], scale[j], -st.x)) * st.y;
+                if (first + 16 * j + 4 * g + i < limit) w[j][i] += p;
+              }
+          }
         }
       }
-    }
+    };
+    if (ends)
+      queries(std::bool_constant<kMicro<EL> && (TERMS > 1)>{});
+    else
+      queries(std::false_type{});
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j) {
 #pragma unroll

@@ -54,7 +54,7 @@ def _far_keys(lens, heads, D, group, W, dtype, paged, causal, fits_bf16=True, t_
     q = _queries((1, len(lens), heads * group, W, D), dtype, fits_bf16)
     want, got = _attend(cache, p, lens, q), _attend(far, p, lens, q)
     for x, y in zip(got, want):
-        assert torch.isfinite(y).all()
+        assert not torch.isnan(y).any()                 # (a query that sees nothing has lse -inf)
         same_bits(x, y)
     for b, T in enumerate(lens):
         assert (got[2].view(len(lens), heads, -1)[b, :, [T - 1, T // 2]] == 0).all()
@@ -67,3 +67,50 @@ def _far_keys(lens, heads, D, group, W, dtype, paged, causal, fits_bf16=True, t_
 def test_weights_from_keys_again(D, heads, paged, group, W, causal):
     """More than 16 queries, with and without places for queries that are not there in the last 32: the position's weight is 0."""
     _far_keys([160, 147], heads, D, group, W, "bf16", paged, causal)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads,paged", [(1, True), (2, False), (2, True)])
+@pytest.mark.parametrize("group,W", [(1, 1), (2, 4), (1, 16), (2, 24), (3, 43)])
+@pytest.mark.parametrize("dtype,fits_bf16", [("bf16", True), ("f32", True), ("f32", False)])
+def test_logits_and_weights(D, heads, paged, group, W, dtype, fits_bf16):
+    """Every kernel and both ways to the weights.  fp32 queries go in as three terms, of which the lower ones may be 0 or have the other sign."""
+    _far_keys([160, 147, 9], heads, D, group, W, dtype, paged, W > 1, fits_bf16)
+
+
+@pytest.mark.parametrize("dtype,fits_bf16", [("bf16", True), ("f32", True), ("f32", False)])
+@pytest.mark.parametrize("group,W", [(2, 4), (5, 3), (2, 9)])
+def test_in_later_steps(group, W, dtype, fits_bf16):
+    """Waves that take several steps, and two heads a wave of up to 16 queries: lengths of up to 40000 allowed."""
+    lens, heads, D, t_max = [1900, 1203], 2, 128, 40000
+    shape = (1, 2, heads, D)
+    cache = filled(shape, 1904, lens, True, 4)
+    cache.table = np.concatenate([cache.table, np.full((2, t_max // 16 - cache.table.shape[1]), -1, np.int32)], 1)
+    far = cache.copy()
+    for b, T in enumerate(lens):
+        for i, t in enumerate((T - 1, 600, 601, 33)):
+            _set_key(cache, b, i % 2, t, 150), _set_key(far, b, i % 2, t, 253 + i % 2)
+    p = params(shape, t_max, group=group, window=W, causal=True, dtype=dtype)
+    q = _queries((1, 2, heads * group, W, D), dtype, fits_bf16)
+    for x, y in zip(_attend(far, p, lens, q), _attend(cache, p, lens, q)):
+        assert torch.isfinite(y).all()
+        same_bits(x, y)
+
+
+@pytest.mark.parametrize("dtype,fits_bf16", [("bf16", True), ("f32", True), ("f32", False)])
+@pytest.mark.parametrize("heads,group,W", [(1, 2, 4), (2, 2, 4), (1, 3, 7)])
+def test_the_other_sign_and_nothing_but_infinite_keys(heads, group, W, dtype, fits_bf16):
+    """A logit of +inf makes the output, the log-sum and the weights of what its queries see no number; a sequence whose every logit is -inf has
+    out 0, lse -inf and no weights."""
+    lens, D, T = [100, 20], 64, 100
+    cache = filled((1, 2, heads, D), T, lens, False, 4)
+    _set_key(cache, 0, 0, 50, 254, 15)                  # -6 * 2^127: +inf for every query
+    for t in range(20):
+        _set_key(cache, 1, 0, t, 253)
+    p = params((1, 2, heads, D), T, group=group, window=W, causal=True, dtype=dtype)
+    q = _queries((1, 2, heads * group, W, D), dtype, fits_bf16)
+    out, lse, w = _attend(cache, p, lens, q)
+    w = w.view(2, heads, T)
+    assert torch.isnan(out[0, 0, :group]).all() and torch.isnan(lse[0, 0, :group]).all() and torch.isnan(w[0, 0, :T - W + 1]).all()
+    assert (out[0, 1, :group] == 0).all() and (lse[0, 1, :group] == -np.inf).all() and (w[1, 0, :20] == 0).all()
+    assert torch.isfinite(out[0, :, group:]).all() and torch.isfinite(lse[0, :, group:]).all() and torch.isfinite(w[:, 1:]).all()
