@@ -238,6 +238,7 @@ int ams_assign_pages(const ams_params* p, const ams_pages* x, const int32_t* len
   if ((int64_t)x->max_blocks_per_seq * kBlockRows < p->t_max) return AMS_ERR_INVALID_ARG;
   if (x->state_out == x->state || lens_out == lens_from || lens_out == lens_to) return AMS_ERR_INVALID_ARG;
   if ((int64_t)p->batch * p->t_max > INT32_MAX) return AMS_ERR_UNSUPPORTED;
+  if (x->max_blocks_per_seq > (1 << 30) || n_slots > (int64_t)1 << 36) return AMS_ERR_UNSUPPORTED;  // (the launch checks their tasks together)
   const PagesArgs a{p->batch, p->t_max, x->max_blocks_per_seq, x->n_pages, lens_from, lens_to, x->table, x->table_out,
                     x->ring, x->state, x->state_out, lens_out, starts, slots, n_slots};
   return status(launch_pages(a, (hipStream_t)stream), (hipStream_t)stream);
