@@ -485,9 +485,9 @@ int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens
  *   starts      [dev] [batch + 1]: the new tokens (max(to - from, 0)) of the sequences before b, or NULL
  *   slots       [dev] [n_slots]: slots[starts[b] + i] = the pool's slot of position from + i of sequence b, page * 16 + position % 16, -1
  *               for a sequence that is not served; -1 from the last token to n_slots; tokens beyond n_slots have none.  NULL with 0
- * Of p: the sizes and t_max, the upper bound of the lengths; max_blocks_per_seq * 16 >= t_max.  AMS_ERR_UNSUPPORTED: batch * t_max from
- * 2^31 on, max_blocks_per_seq above 2^30, n_slots above 2^36, batch * ceil(max_blocks_per_seq / 128) + ceil(n_slots / 64) from 2^31 on.
- * One table serves all layers.  The names in ring and table are taken as they are.
+ * Of p: batch and t_max, the upper bound of the lengths (one table serves all layers and heads); max_blocks_per_seq * 16 >= t_max.
+ * AMS_ERR_UNSUPPORTED: batch above 2^20, t_max above 2^30, batch * t_max from 2^31 on, max_blocks_per_seq above 2^30, n_slots above 2^36,
+ * batch * ceil(max_blocks_per_seq / 128) + ceil(n_slots / 64) from 2^31 on.  The names in ring and table are taken as they are.
  */
 typedef struct {
   const int32_t* table;

@@ -23,6 +23,12 @@ int check_sizes(const ams_params* p) {
   if ((int64_t)p->n_kv_heads * p->group > 65535 || p->t_max > (1 << 30)) return AMS_ERR_UNSUPPORTED;
   return AMS_OK;
 }
+// Of a table that serves all layers and heads.  (2^20 sequences: sums over them stay inside 32 bits whatever t_max is.)
+int check_pages(const ams_params* p) {
+  if (!p || p->batch < 1 || p->t_max < 1) return AMS_ERR_INVALID_ARG;
+  if (p->batch > (1 << 20) || p->t_max > (1 << 30)) return AMS_ERR_UNSUPPORTED;
+  return (int64_t)p->batch * p->t_max > INT32_MAX ? AMS_ERR_UNSUPPORTED : AMS_OK;
+}
 int check_attend(const ams_params* p) {
   const int rc = check_sizes(p);
   if (rc) return rc;
@@ -231,13 +237,12 @@ int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens
 
 int ams_assign_pages(const ams_params* p, const ams_pages* x, const int32_t* lens_from, const int32_t* lens_to, int32_t* lens_out,
                      int32_t* starts, int64_t* slots, int64_t n_slots, void* stream) {
-  const int rc = check_sizes(p);
+  const int rc = check_pages(p);
   if (rc) return rc;
   if (!x || !x->table || !x->table_out || !x->ring || !x->state || !x->state_out || !lens_from || !lens_to) return AMS_ERR_INVALID_ARG;
   if (x->max_blocks_per_seq < 1 || x->n_pages < 1 || n_slots < 0 || (n_slots > 0 && !slots)) return AMS_ERR_INVALID_ARG;
   if ((int64_t)x->max_blocks_per_seq * kBlockRows < p->t_max) return AMS_ERR_INVALID_ARG;
   if (x->state_out == x->state || lens_out == lens_from || lens_out == lens_to) return AMS_ERR_INVALID_ARG;
-  if ((int64_t)p->batch * p->t_max > INT32_MAX) return AMS_ERR_UNSUPPORTED;
   if (x->max_blocks_per_seq > (1 << 30) || n_slots > (int64_t)1 << 36) return AMS_ERR_UNSUPPORTED;  // (the launch checks their tasks together)
   const PagesArgs a{p->batch, p->t_max, x->max_blocks_per_seq, x->n_pages, lens_from, lens_to, x->table, x->table_out,
                     x->ring, x->state, x->state_out, lens_out, starts, slots, n_slots};

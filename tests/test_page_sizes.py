@@ -17,3 +17,9 @@ def test_tables_and_slots_beyond_what_is_counted(kw):
                                       (130, dict(max_blocks_per_seq=1 << 30, n_slots=1 << 36))])
 def test_together_too_many(batch, kw):
     assert _pages(_p(n_layers=1, batch=batch, n_kv_heads=1), **kw) == B.ERR_UNSUPPORTED
+
+
+def test_batches():
+    assert _pages(_p(batch=(1 << 20) + 1, t_max=16, t_stride=16)) == B.ERR_UNSUPPORTED
+    assert _pages(_p(batch=-1)) == B.ERR_INVALID_ARG and _pages(_p(t_max=0)) == B.ERR_INVALID_ARG
+    assert _pages(_p(t_max=(1 << 30) + 1, batch=1), max_blocks_per_seq=1 << 30) == B.ERR_UNSUPPORTED
