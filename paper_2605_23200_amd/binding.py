@@ -92,14 +92,12 @@ _lib = None
 
 
 def lib() -> C.CDLL:
-    """Loads the built library and the checks of tensor arguments; raises if they have not been built (no fallback exists)."""
-    global _lib, _arg, _token_rows
+    """Loads the built library; raises if it has not been built (no fallback exists)."""
+    global _lib
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise ImportError(f"{LIB_PATH} is missing: run `python -m paper_2605_23200_amd.build` "
                               "(or __graft_entry__.build()) first")
-        from . import _args
-        _arg, _token_rows = _args.arg, _args.token_rows
         l = C.CDLL(LIB_PATH)
         l.ams_status_string.restype = C.c_char_p
         l.ams_status_string.argtypes = [C.c_int]
@@ -310,15 +308,27 @@ def _cache_for(p: Params, c: Cache):
     return c.index
 
 
+def _load_args():
+    """The compiled checks of tensor arguments (csrc/args.cpp) in the place of the two functions below, which the first use of either calls.  A module
+    of this torch and Python: the entry points that do not use it do not need it."""
+    global _arg, _token_rows
+    try:
+        from . import _args
+    except ImportError as e:
+        raise ImportError(f"{os.path.join(_HERE, '_args.so')} is missing or was built for another torch or Python: run "
+                          "`python -m paper_2605_23200_amd.build` (or __graft_entry__.build())") from e
+    _arg, _token_rows = _args.arg, _args.token_rows
+
+
 def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, gpu: int, what: str):
-    """Pointer of a contiguous tensor of at least `numel` elements on that GPU; None stays None.  (Compiled, csrc/args.cpp: lib() puts it here.)"""
-    lib()
+    """Pointer of a contiguous tensor of at least `numel` elements on that GPU; None stays None."""
+    _load_args()
     return _arg(t, dtype, numel, gpu, what)
 
 
 def _token_rows(t: torch.Tensor, shape, dtype: torch.dtype, gpu: int, what: str):
-    """(pointer, elements from token to token) of [L, B, n_new, heads, D]: any slice of a projection's output along the heads.  (Compiled as well.)"""
-    lib()
+    """(pointer, elements from token to token) of [L, B, n_new, heads, D]: any slice of a projection's output along the heads."""
+    _load_args()
     return _token_rows(t, shape, dtype, gpu, what)
 
 

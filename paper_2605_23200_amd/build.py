@@ -54,11 +54,11 @@ def build(jobs: int = 6) -> str:
     with ThreadPoolExecutor(max_workers=jobs) as ex:
         args = ex.submit(_compile_args)
         objs = list(ex.map(_compile, SOURCES))
-        args.result()
     r = subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs],
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
+    args.result()  # (last: where it fails the library is there for the entry points that do not use it)
     return LIB
 
 
