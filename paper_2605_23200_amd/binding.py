@@ -250,8 +250,14 @@ def ams_compress_step(p, src, seq_lens, q, credit, dst, credit_dst, idx, n_kept,
 
 # ---- between two events: new rows, attention, eviction, caches in 8 and 4 bits, pages ----
 
-_CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: INT8, torch.float8_e4m3fn: E4M3, torch.uint8: E2M1,
-                 torch.float4_e2m1fn_x2: E2M1}
+def _types(*names):
+    """Those of torch's types that this torch has (those of 4 bits and of their scales came late; uint8 stands for either)."""
+    return tuple(getattr(torch, n) for n in names if hasattr(torch, n))
+
+
+_CACHE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.int8: INT8, torch.float8_e4m3fn: E4M3,
+                 **dict.fromkeys(_types("uint8", "float4_e2m1fn_x2"), E2M1)}
+_SCALE_DTYPES = {INT8: (torch.float32,), E4M3: (torch.float32,), E2M1: _types("uint8", "float8_e8m0fnu")}
 BLOCK = 16                             # positions that share a scale (in 4 bits: whose scales lie together); a page
 MICRO = 32                             # channels of a row that share a scale in 4 bits
 
@@ -275,8 +281,8 @@ def cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor]
         raise ValueError("k and v: one shape, one element type of bf16, fp32, int8, float8_e4m3fn, uint8, float4_e2m1fn_x2; "
                          "five dimensions, paged four")
     dtype = _CACHE_DTYPES[k.dtype]
-    if dtype in (INT8, E4M3, E2M1):
-        kinds = (torch.uint8, torch.float8_e8m0fnu) if dtype == E2M1 else (torch.float32,)
+    if dtype in _SCALE_DTYPES:
+        kinds = _SCALE_DTYPES[dtype]
         for t in (k_scale, v_scale):
             if t is None or t.dtype not in kinds or tuple(t.shape) != scale_shape(k):
                 raise ValueError(f"{' or '.join(str(t) for t in kinds)} scales of shape {scale_shape(k)} expected")

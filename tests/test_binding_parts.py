@@ -54,3 +54,21 @@ def test_the_library_is_linked_where_the_checks_do_not_compile(monkeypatch, tmp_
     with pytest.raises(RuntimeError, match="args.cpp"):
         build.build()
     assert done[-1] == "hipcc" and sorted(done[:-1]) == sorted(build.SOURCES)
+
+
+def test_a_torch_without_types_of_4_bits():
+    """uint8 codes and scales need no type of torch's own."""
+    assert _python("""
+import torch
+for name in ("float4_e2m1fn_x2", "float8_e8m0fnu"):
+    delattr(torch, name)
+from paper_2605_23200_amd import binding as B
+print(B.scale_shape(torch.empty((2, 3, 4, 100, 64), dtype=torch.uint8)), B._SCALE_DTYPES[B.E2M1], B._SCALE_DTYPES[B.INT8])
+""") == "(2, 3, 4, 7, 4, 16) (torch.uint8,) (torch.float32,)".split()
+
+
+def test_the_types_that_this_torch_has():
+    import torch
+    from paper_2605_23200_amd import binding as B
+    assert B._CACHE_DTYPES[torch.float4_e2m1fn_x2] == B._CACHE_DTYPES[torch.uint8] == B.E2M1
+    assert B._SCALE_DTYPES[B.E2M1] == (torch.uint8, torch.float8_e8m0fnu) and set(B._SCALE_DTYPES) == {B.INT8, B.E4M3, B.E2M1}
