@@ -412,7 +412,8 @@ typedef struct {
  * the call begins takes nothing from its old scale.
  *   q_out    [dev] [layers, batch, kv_heads * group, n_new, head_dim] kv_dtype, all of it written; not x->q; NULL when
  *            x->q is
- *   lens_out [dev] [batch] min(seq_lens[b] + n_new, t_max), or NULL; not seq_lens itself
+ *   lens_out [dev] [batch] min(seq_lens[b] + n_new, t_max), or NULL; not seq_lens itself.  It counts rows whose block has no page in
+ *            the table (never written): sequences that ams_assign_pages did not serve are to be left out
  * rope NULL or rot_dim 0: no rotation.
  */
 int ams_append(const ams_params* p, const ams_new_tokens* x, const ams_rope* rope, const int32_t* seq_lens, void* q_out,
@@ -481,7 +482,8 @@ int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens
  *   table, table_out  [dev] [batch, max_blocks_per_seq]; entries behind a sequence's pages are -1 in table_out and not read in table; may
  *               be the same array
  *   ring        [dev] [n_pages], updated; state, state_out [dev] [2], not the same array
- *   lens_out    [dev] [batch] to, or from where the sequence is not served; NULL; not lens_from or lens_to
+ *   lens_out    [dev] [batch] to, or from where the sequence is not served: what the caller goes on with, leaving out what was not
+ *               served (seq_lens[b] = t_max in ams_append, 0 in ams_attend); NULL; not lens_from or lens_to
  *   starts      [dev] [batch + 1]: the new tokens (max(to - from, 0)) of the sequences before b, or NULL
  *   slots       [dev] [n_slots]: slots[starts[b] + i] = the pool's slot of position from + i of sequence b, page * 16 + position % 16, -1
  *               for a sequence that is not served; -1 from the last token to n_slots; tokens beyond n_slots have none.  NULL with 0
