@@ -158,7 +158,10 @@ AttendLayout attend_layout(const ams_params* p, bool pairs) {
   // 64 units of 32768 and 32 queries: 201, 187, 178, 172 (the last is one round).
   // Pairs of heads (4 bits): one on a CU, with twice the loads in flight (one, two, three, four on a CU: 4 units of 131072 26, 27, 31, 33 us;
   // 32 units of 16384 23.3, 24.2, 25.9, 27.0, ragged ones 22.4, 22.1, 24.5, 24.3; 128 of 8192 45, 48, 51, 49, ragged ones 35, 34, 31, 35).  That
-  // is never more splits than head by head, so the workspace for any cache is that of one head at a time.
+  // is never more splits than head by head, so the workspace for any cache is that of one head at a time.  Where one round leaves a quarter of
+  // the CUs or more without a workgroup, 512 positions again, in no more splits than head by head: 264 units of 7000 91 -> 78 us, ragged ones
+  // 86 -> 55; 264 of 4096 57 -> 53 and 53 -> 34, 320 60 -> 58 and 54 -> 39, 384 66 -> 68 and 56 -> 49; 176 of 10000 79 -> 74 and 69 -> 55.
+  // Not where more have one: 224 units of 4096 38.6 and 41.2 us, 480 77 and 85.
   r.pairs = pairs;
   const size_t per_split = units * r.row_groups / (pairs ? 2 : 1), resident = pairs ? 1 : (r.row_tiles == 1 ? 3 : 2) - (p->kv_dtype == AMS_F32 && p->head_dim == 128);
   const int fine = r.row_tiles == 1 ? 512 : 2048;
@@ -167,6 +170,8 @@ AttendLayout attend_layout(const ams_params* p, bool pairs) {
   } else {
     const int splits = (int)max((size_t)1, 256 * resident / per_split);
     r.chunk = div_up(div_up(p->t_max, splits), kWaves * kStep) * kWaves * kStep;
+    if (pairs && 4 * splits * per_split <= 3 * 256)
+      r.chunk = max(fine, div_up(div_up(p->t_max, attend_layout(p, false).n_splits), kWaves * kStep) * kWaves * kStep);
   }
   while (div_up(p->t_max, r.chunk) > 4096) r.chunk *= 2;  // what the join goes through
   r.n_splits = div_up(p->t_max, r.chunk);
