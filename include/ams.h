@@ -475,7 +475,7 @@ int ams_evict(const ams_params* p, const ams_cache* src, const int32_t* seq_lens
  * ams_assign_pages - block tables, slots of new tokens and the free pages of a pool, from the rows that every sequence has and is to
  * have.  A pool's free pages are a ring: `count` names from ring[head] on, round the end of its n_pages places; state = {head, count}.  (A
  * new pool: ring = 0 .. n_pages - 1, state = {0, n_pages}.)
- * With from = lens_from[b] and to = lens_to[b] a sequence keeps its first ceil(from / 16) pages; where to needs more, it takes them
+ * With from = lens_from[b] and to = lens_to[b] (each taken into 0 .. t_max) a sequence keeps its first ceil(from / 16) pages; where to needs more, it takes them
  * from the front of the ring, sequences in order, and where to needs fewer, those behind go to the end of the ring, in order of
  * (sequence, place).  Pages that go back in a call are given out from the next call on.  A sequence that the free pages do not
  * suffice for stays as it was, and so do those behind it that ask for pages; the others are served.

@@ -9,15 +9,17 @@
 // exchange, and four cosines and sines in one LDS read each.  (Eight channels in a row, with the other halves and interleaved
 // cosines and sines out of LDS, took 35 us for 2036 tokens of 48 heads against 23: every read hit the same banks.)  Halves that are no
 // multiple of four channels find the other channel in LDS.
-// What bounds it: a launch and its chain of latencies for single tokens (5 us for one, 7 for 64 sequences); 64-bit arithmetic of the
-// keys for long pieces (17 us for 2036 tokens of 48 heads to 8 bits, of 10 that the bytes take; 25 for 4096 tokens to bf16, 2048 each).
+// What bounds it: a launch and its chain of latencies for single tokens (5 us for one, 7 for 64 sequences).  For long pieces a wave's heads,
+// whose loads, instructions and stores come one after the other (the next head's rows are loaded into the registers of this one's): 2036
+// tokens of 48 heads to 8 bits take 17 us, of 10 that the bytes take; the vector ALU is active for 55 % of the time and waves wait for 52 % of
+// theirs, at three waves on a SIMD.  Keys in 64 bits are 3 of the 17.  4096 tokens to bf16, 2048 each: 25 us.
 // Angles: position * (frequency / 2 pi) in 64 bits, whole turns taken off there: at position 10^6 fp32 would be off by 0.06 rad.
 // Keys that go to 8 or 4 bits are normalised and rotated in 64 bits: a code changes by a whole step where the value
 // crosses the middle between two, and fp32 takes about one key element in a million across.
 // 4 bits: every row has its own scales, one for 32 channels, whose eight runs of four the rotation leaves in any of the row's lanes: the
-// largest magnitudes of the runs go through LDS.  One token 5.5 us, 2036 tokens of 48 heads 18.8.  (Keys in 32 bits with a bound, and in 64 only
-// where a code may hang on it: with the rows read back 28.5 instead of 22.2, and 21.1 with the second path taken out: the 64 bits are not what
-// costs.)
+// largest magnitudes of the runs go through LDS.  One token 5.5 us, 2036 tokens of 48 heads 19: active for 57 %, waiting for 48 %, the 64 bits 2.4
+// of it (all keys in 32 bits would turn codes).  (Keys in 32 bits with a bound, and in 64 only where a code may hang on it:
+// with the rows read back 28.5 instead of 22.2.)
 #include "cache.h"
 
 namespace ams {

@@ -15,7 +15,8 @@
 // 63 for 64 sequences of up to 4096, and 62 instead of 59 for 16 of up to 16384.  (512 workgroups that each take an even share of all
 // positions: 218; three waves on a SIMD: 218.)  64 channels: half lines also two heads at a time, 157 us against 134 for slabs.
 // 9 to 16 queries a head: the same tiles of K with the 16 columns of either head in turn, P and Q likewise: twice the products, none of the
-// logits wasted.  64 ragged sequences of up to 16384 positions and 14 queries: a pass of 321 us, 362 head by head (306 in slabs).
+// logits wasted.  64 ragged sequences of up to 16384 positions and 14 queries: a pass of 321 us, 362 head by head (306 in slabs).  222 of it are
+// this kernel (vector ALU active for 54 %, matrix cores for 28 %, 24 % of the wave cycles waiting), 99 the join of its logits.
 #include "attend_kernel.h"
 
 namespace ams {

@@ -21,9 +21,11 @@
 // LDS: 52; the masks as a variant of the step: 44, but 128 against 120 for 64 units and 32 queries.)
 //
 // Codes of 4 bits: a quarter of a row of K is of one scale and in one lane, a conversion of two codes multiplies by the scale as well, and the
-// values are bf16 numbers, so that logits and probabilities need no factors; the rest is the same.  (Up to 16 queries: attend_e2m1.hip.)  64
+// values are bf16 numbers, so that logits and probabilities need no factors; the rest is the same.  (Pairs of heads run in attend_e2m1.hip: up to 8
+// queries, and 9 to 16 of bf16 over 128 channels in pages with positions enough; odd head counts, slabs of 2^24 rows and the other calls of 9 to 16
+// queries run here, as all of more.)  64
 // ragged sequences of up to 16384 positions and 14 queries a head in slabs: 306 us; 8 units of 32768 and 128 queries: 39 us (345 vector
-// instructions for 32 positions and 32 queries, vector ALU 57 %, matrix cores 28 %; with 64 queries a wave 54; with three waves on a SIMD,
+// instructions for 32 positions and 32 queries, vector ALU active for 57 %, matrix cores for 28 %; with 64 queries a wave 54; with three waves on a SIMD,
 // which spill 30 registers, a pass of 61 takes 67).  Not with the matrix cores' own scaled products of 4-bit by 8-bit floats, which take K's codes as they are: inside 32
 // channels their sums lose what lies about 2^14 below the largest product (5e-4 of it for codes of any size, measured), and queries would have
 // to go in as several terms of 4 bits.
@@ -64,7 +66,8 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t w) {
     return __builtin_bit_cast(uint32_t, c);
   }
 }
-// Eight of 4 bits, of the scale 2^(byte - 127) whose byte is the exponent of `scale`: byte 255 makes all of them no number, 0 is 2^-127.
+// Two codes of 4 bits of a word, those of its byte `byte`, as bf16; their scale is 2^(x - 127), x the exponent bits of `scale`: 255 makes both no
+// number, 0 is 2^-127.
 __device__ __forceinline__ uint32_t two_of_four_bits(uint32_t w, float scale, int byte) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   bf16x2 c;
@@ -80,7 +83,7 @@ __device__ __forceinline__ uint32_t two_of_four_bits(uint32_t w, float scale, in
 constexpr uint32_t kBeyond = 253u << 23;  // as the scale's bits
 // Those of an operand as 0.  Queries of fp32 go in as three terms, of which the lower ones may be 0 or have the other sign: times an infinite
 // key they would make a logit no number that the first term makes infinite.  (So products are formed in two ways, by whether a step holds such
-// a scale: 8 units of 16384 and 128 queries 65.5 -> 66.2 us, 16.4 us and less no difference.)
+// a scale: 8 units of 16384 and 128 queries 65.5 -> 66.2 us; up to 32 queries no difference.)
 __device__ __forceinline__ bf16x8 without_infinite(bf16x8 x) {
   uint4 r = __builtin_bit_cast(uint4, x);
   asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w));  // (formed where it is used: kept over a loop it would take 64 registers)
@@ -203,7 +206,8 @@ struct Queries {
   }
 };
 
-// Loads of what no kernel here writes and every lane of the wave wants: through the scalar cache.
+// Loads of what this kernel does not write and every lane of the wave wants (a block table, scales; other launches write them): through the
+// scalar cache.
 template <typename T>
 __device__ __forceinline__ T uniform_load(const T* p) {
   return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
@@ -655,7 +659,8 @@ __global__ __launch_bounds__(kThreads, R == 1 ? (BF16 || HD == 64 ? 3 : 2) : (BF
 // blocks of positions at a time, converts them once, runs 32 queries at a time over them, and has the next two on their way.  (One step per
 // workgroup, with the queries loaded for it, is latency: 172 us for 64 units of 32768 positions and 32 queries, 80 with several.)
 // With fp32 queries four blocks, so that their three terms come out of LDS half as often (a pass of 8 units of 16384 and 128 queries
-// 64 us, 69 with two blocks; bf16, 64 units of 32768 and 32 queries 214 with four blocks at two workgroups on a CU, 201 with two at four).
+// 64 us, 69 with two blocks; bf16, 64 units of 32768 and 32 queries 214 with four blocks at two workgroups on a CU, 201 with two at four; a
+// pass of 8 units of 32768 and 128 queries in 4 bits 62, 65 and 67 with two, three and four).
 constexpr int kWeightRows = 32;
 template <bool BF16>
 constexpr int kWeightBlocks = BF16 ? 2 : 4;

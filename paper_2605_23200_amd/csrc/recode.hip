@@ -11,8 +11,9 @@
 // 4 bits: a scale for every 32 channels of a row, which are four lanes; no two rows have anything in common.  2048 of 32768 bf16 rows, 256
 // units: 95 us, and 60 back to rows, 680 MB in all at 4.4 TB/s (92 with a conversion that does nothing, 47 without its stores: while it
 // reads, the memory-side cache writes back what the kernel before it wrote).  Four or five waves on a SIMD instead of eight win 3 % of that and
-// lose 2 % with whole slabs.  4 bits to 4 bits, 2048 of up to 16384 rows of 64 bytes scattered over a pool: 62 us with the write-back of 268 MB
-// (one, two and four rows a lane in flight: 151, 153 and 157 us for the eviction and its reading back).
+// lose 2 % with whole slabs.  4 bits to 4 bits, 2048 of up to 16384 rows of 64 bytes scattered over a pool, 159 MB: 40 us (4.0 TB/s) where the caches hold
+// nothing that waits to be written, 45 after its own last pass, 63 after a kernel that wrote 268 MB of bf16 rows (an eviction that is read back).
+// (One, two and four rows a lane in flight: 151, 153 and 157 us for the eviction and its reading back.)
 #include "cache.h"
 
 namespace ams {
