@@ -100,8 +100,8 @@ def test_in_later_steps(group, W, dtype, fits_bf16):
 @pytest.mark.parametrize("dtype,fits_bf16", [("bf16", True), ("f32", True), ("f32", False)])
 @pytest.mark.parametrize("heads,group,W", [(1, 2, 4), (2, 2, 4), (1, 3, 7)])
 def test_the_other_sign_and_nothing_but_infinite_keys(heads, group, W, dtype, fits_bf16):
-    """A logit of +inf makes the output, the log-sum and the weights of what its queries see no number; a sequence whose every logit is -inf has
-    out 0, lse -inf and no weights."""
+    """A logit of +inf makes the output and the weights of what its queries see no number, and their log-sum not finite; a sequence whose every logit
+    is -inf has out 0, lse -inf and no weights."""
     lens, D, T = [100, 20], 64, 100
     cache = filled((1, 2, heads, D), T, lens, False, 4)
     _set_key(cache, 0, 0, 50, 254, 15)                  # -6 * 2^127: +inf for every query
@@ -111,6 +111,6 @@ def test_the_other_sign_and_nothing_but_infinite_keys(heads, group, W, dtype, fi
     q = _queries((1, 2, heads * group, W, D), dtype, fits_bf16)
     out, lse, w = _attend(cache, p, lens, q)
     w = w.view(2, heads, T)
-    assert torch.isnan(out[0, 0, :group]).all() and torch.isnan(lse[0, 0, :group]).all() and torch.isnan(w[0, 0, :T - W + 1]).all()
+    assert torch.isnan(out[0, 0, :group]).all() and not torch.isfinite(lse[0, 0, :group]).any() and torch.isnan(w[0, 0, :T - W + 1]).all()
     assert (out[0, 1, :group] == 0).all() and (lse[0, 1, :group] == -np.inf).all() and (w[1, 0, :20] == 0).all()
     assert torch.isfinite(out[0, :, group:]).all() and torch.isfinite(lse[0, :, group:]).all() and torch.isfinite(w[:, 1:]).all()
